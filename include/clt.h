@@ -252,6 +252,103 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
                            int64_t t, float lr, const clt_tensors* params, const clt_tensors* grads,
                            const clt_tensors* m, const clt_tensors* v, const clt_tensors* master);
 
+/* ---- Around the training step: its 8-bit inputs, an optimiser in 8 bits, the encoder in 4 bits -------------------
+ *
+ * The functions of this part need no handle and no workspace of one; they allocate nothing, do not synchronise, may be
+ * captured into a HIP graph, and report errors through clt_last_error(NULL).  Calls on different streams may overlap as
+ * long as they do not share what they write. */
+
+/* Root-mean-square norm of residual streams, as a decoder-only language model applies it in front of an MLP: the
+ * activations x[L,B,d] that a transcoder reads (Sec. 3.1 caches them).  Per row of d elements, all in fp32:
+ *   h = x + residual, rounded to T (without residual: h = x);   rstd = 1 / sqrt(mean(h^2) + eps);
+ *   y = h rstd weight[l].
+ * residual: [L,B,d] T or NULL.  h: where the sum is stored, [L,B,d] T; required with residual (it may be x or residual
+ * itself), NULL without.  weight: [L,d] float.  Outputs, at least one of the first two: y [L,B,d] T; q [L,B,d] int8 with
+ * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
+ * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
+ * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN gets codes 0 and a NaN as its scale.
+ * Except for h, an output must not overlap an input.  L, B >= 1, d a positive multiple of 8, eps > 0. */
+int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
+                 const float* weight, float eps, void* h, void* y, int8_t* q, float* q_scale, float* rstd);
+
+/* Backward pass of clt_rms_norm (through int8 codes: straight through).  h is what was normalised (the stored sum, or x where
+ * there was no residual), rstd as the forward pass wrote it, dy the gradient of y, dh the gradient that reaches h past the
+ * norm (NULL: none):
+ *   dx = rstd (weight dy) - h rstd^3 mean(weight dy h) + dh,    dweight[l] = sum over the B rows of dy h rstd.
+ * dx [L,B,d] T is the gradient of both x and residual; it may be dy or dh.  dweight: [L,d] float, or NULL when the
+ * weights are not trained; with it, workspace (device, 16-byte aligned) of at least
+ * clt_rms_norm_backward_workspace_bytes bytes, which nothing has to clear.  Sums in fp32, in a fixed order. */
+int clt_rms_norm_backward_workspace_bytes(int32_t L, int32_t B, int32_t d, size_t* bytes);
+int clt_rms_norm_backward(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* h, const float* weight,
+                          const float* rstd, const void* dy, const void* dh, void* dx, float* dweight, void* workspace,
+                          size_t workspace_bytes);
+
+/* One tensor of clt_adamw_step, n >= 0 elements, contiguous.  Moments in 32 bits: m, v float, m_scale and v_scale NULL.
+ * Moments in 8 bits, in blocks of CLT_ADAMW_BLOCK consecutive elements (the last one may be shorter), each with a
+ * power of two 2^(s-127) of its own, s one byte in m_scale / v_scale (ceil(n / CLT_ADAMW_BLOCK) bytes each; the OCP
+ * formats E4M3 for m, E5M2 for v, E8M0 for the scales): value = element * 2^(s-127).  All bytes 0 is a state of
+ * zeros.  A block whose new moments hold an infinity or a NaN (a gradient did) gets s = 255: all its values are NaN
+ * from then on, so that a broken step shows instead of being rounded away. */
+#define CLT_ADAMW_BLOCK 128
+typedef struct clt_adamw_tensor {
+  void* p;             /* parameters, dtype                                         */
+  const void* g;       /* gradient, grad_dtype                                      */
+  void* m;             /* first moment: float or E4M3 bytes                         */
+  void* v;             /* second moment: float or E5M2 bytes                        */
+  uint8_t* m_scale;    /* 8-bit moments only                                        */
+  uint8_t* v_scale;
+  float* master;       /* fp32 copy that is updated and rounded into p, or NULL     */
+  int64_t n;
+  int32_t dtype;       /* CLT_DTYPE_F32 or CLT_DTYPE_BF16                           */
+  int32_t grad_dtype;  /* CLT_DTYPE_F32 or CLT_DTYPE_BF16                           */
+  int32_t state_bits;  /* 32 or 8                                                   */
+  float weight_decay;  /* of this tensor, >= 0                                      */
+} clt_adamw_tensor;
+
+/* One AdamW step (Adam as in clt_adam_step, plus decoupled weight decay) over a list of tensors of any sizes and types,
+ * in one launch for every 32 of them:
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + ((1 - beta2) g) g,
+ *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^t) m' / (sqrt(v' / (1 - beta2^t)) + eps).
+ * The update uses m' and v' before they are rounded.  8-bit moments are rounded to one of their two neighbours at
+ * random, without bias: with beta2 = 0.999, v moves by a thousandth of itself in a step and a step of E5M2 is 14 to 25 %, so
+ * that rounding to nearest would never let it move; and because the scales are powers of two, a value that stays
+ * keeps its neighbours from step to step, and the noise stays near the square root of (step x drift).  The random
+ * bits are a function of (seed, t, position in the list, element), so a step can be repeated bit for bit; a v' above
+ * zero never rounds to zero.  t >= 1 is the step count, lr >= 0, 0 <= beta < 1, eps > 0 (doubles, so that 1 - beta and
+ * the bias corrections are formed before they are rounded to float).  Tensors must not overlap. */
+int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tensors, int64_t t, double lr, double beta1,
+                   double beta2, double eps, uint64_t seed);
+
+/* Matrices in 4-bit microscaled floating point (OCP MXFP4): elements E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives), and for every 32 consecutive elements along the contraction a power of two 2^(s-127), s one byte (E8M0).
+ * s is the smallest for which no element is off by more than half a step: with max|a| = 2^e f, 1 <= f < 2, s - 127 = e - 2 for
+ * f < 1.75 and e - 1 above (not below 2^-127).  Elements are rounded to nearest, ties to even.  A block with an infinity or a
+ * NaN gets s = 255: its products are NaN.
+ *
+ * A packed matrix of [L][rows][K] (K along the contraction) is two arrays, in the order in which the matrix cores read
+ * them; KS = ceil(K / 128) steps, RP = ceil(rows / 64) panels:
+ *   codes   [L][4 RP][KS][4 blocks of 32][16 rows][16 bytes]: element k of a block in byte k / 2, even k in the low half
+ *   scales  [L][RP][KS][4 blocks of 32][16 rows][4]: row r of a panel at [r % 16][r / 16]
+ * The elements of a row from K up to 128 KS are zeros.  Rows beyond `rows` are room that is never written and whose contents
+ * reach no result.  K is a positive multiple of 8. */
+int clt_mx4_bytes(int32_t L, int32_t rows, int32_t K, size_t* codes_bytes, size_t* scales_bytes);
+
+/* Packs a: [L][rows][K] of T or, with CLT_INPUT_INT8_ROWSCALE (dtype bf16), int8 codes times a_scale [L][rows]; with
+ * transposed != 0, a is [L][K][rows] of T (W_enc [L,d,F] with rows = F, K = d), rows a multiple of 8. */
+int clt_mx4_quantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t dtype, int32_t input_format, int32_t transposed,
+                     const void* a, const float* a_scale, void* codes, void* scales);
+
+/* The values of a packed matrix, out [L][rows][K] of T. */
+int clt_mx4_dequantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t dtype, const void* codes, const void* scales,
+                       void* out);
+
+/* out[l] = A[l] B[l]^T + bias[l], with theta kept where it is > theta[l] and 0 elsewhere: with A the packed activations
+ * (M tokens) and B the packed W_enc (N = F features), the encoder and JumpReLU of eq. 1 on 4-bit operands, for passes that
+ * only need features.  A is [L][M][K], B [L][N][K], bias and theta [L][N] float or NULL, out [L][M][N] of T; N a
+ * multiple of 8.  Accumulated in fp32; the comparison is made before the rounding to T. */
+int clt_mx4_product(void* stream, int32_t L, int32_t M, int32_t N, int32_t K, const void* a_codes, const void* a_scales,
+                    const void* b_codes, const void* b_scales, const float* bias, const float* theta, int32_t dtype, void* out);
+
 /* Device pointers into the workspace, for inspection by tests and tools:
  * which = 0 decoder norms [L,F] float; 1 d y_hat [L,B,d] T; 2 d pre [L,B,F] T
  * (with int8 inputs every row holds d pre times that row's x_scale: the form

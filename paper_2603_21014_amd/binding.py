@@ -25,7 +25,9 @@ DECODE_AUTO, DECODE_DENSE, DECODE_GATHER = 0, 1, 2
 EXPORTS = ("clt_workspace_bytes", "clt_init", "clt_destroy", "clt_last_error", "clt_forward",
            "clt_loss", "clt_backward", "clt_adam_step", "clt_backward_adam_step", "clt_workspace_view",
            "clt_profile_enable", "clt_profile_num_kernels", "clt_profile_query", "clt_norm_accumulate",
-           "clt_normalise", "clt_diag_mfma_loop", "clt_norm_accumulate_static")
+           "clt_normalise", "clt_diag_mfma_loop", "clt_norm_accumulate_static", "clt_rms_norm",
+           "clt_rms_norm_backward_workspace_bytes", "clt_rms_norm_backward", "clt_adamw_step", "clt_mx4_bytes",
+           "clt_mx4_quantise", "clt_mx4_dequantise", "clt_mx4_product")
 
 
 class CLTError(RuntimeError):
@@ -47,6 +49,12 @@ class clt_config(C.Structure):
 class clt_tensors(C.Structure):
     _fields_ = [("W_enc", C.c_void_p), ("b_enc", C.c_void_p), ("theta", C.c_void_p),
                 ("W_dec", C.c_void_p), ("b_dec", C.c_void_p)]
+
+
+class clt_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("master", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("weight_decay", C.c_float)]
 
 
 def _load():
@@ -73,6 +81,16 @@ def _load():
                                       C.POINTER(C.c_int64)]
     lib.clt_norm_accumulate_static.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, fp, vp]
     lib.clt_diag_mfma_loop.argtypes = [vp, C.c_int, C.c_int, vp, C.c_size_t, vp, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    i32, size_p = C.c_int32, C.POINTER(C.c_size_t)
+    lib.clt_rms_norm.argtypes = [vp, i32, i32, i32, i32, vp, vp, fp, C.c_float, vp, vp, vp, fp, fp]
+    lib.clt_rms_norm_backward_workspace_bytes.argtypes = [i32, i32, i32, size_p]
+    lib.clt_rms_norm_backward.argtypes = [vp, i32, i32, i32, i32, vp, fp, fp, vp, vp, vp, fp, vp, C.c_size_t]
+    lib.clt_adamw_step.argtypes = [vp, i32, C.POINTER(clt_adamw_tensor), C.c_int64, C.c_double, C.c_double, C.c_double,
+                                   C.c_double, C.c_uint64]
+    lib.clt_mx4_bytes.argtypes = [i32, i32, i32, size_p, size_p]
+    lib.clt_mx4_quantise.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, fp, vp, vp]
+    lib.clt_mx4_dequantise.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
+    lib.clt_mx4_product.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, fp, fp, i32, vp]
     for n in EXPORTS:
         if n != "clt_last_error":
             getattr(lib, n).restype = C.c_int
@@ -274,6 +292,176 @@ def clt_backward_adam_step(H: Handle, x, z, act_class, t: int, lr: float, params
     _check(rc, H.h)
 
 
+# ---- around the training step: no handle ------------------------------------------------------------------------
+
+def _storage(t, name):
+    """(dtype code, torch dtype) of a native activation or matrix tensor [L, B, d], which sets the type of the call."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: expected a 3-dimensional float32 or bfloat16 tensor, got {tuple(t.shape)} {t.dtype}")
+    return (DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16), t.dtype
+
+
+def _here(*tensors):
+    """The kernels run on the current device's current stream: every tensor has to live there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def clt_rms_norm(x, weight, eps, y=None, q=None, q_scale=None, residual=None, h=None, rstd=None):
+    """RMS norm of residual streams x (+ residual, the sum stored in h) into y and / or int8 codes q with row scales
+    q_scale (include/clt.h).  x [L, B, d] float32 or bfloat16, weight [L, d] float32; rstd [L, B] for the backward pass."""
+    dt, T = _storage(x, "x")
+    f32, s = torch.float32, tuple(x.shape)
+    args = (dt, _ptr(x, s, T, "x"), _ptr(residual, s, T, "residual", True), _ptr(weight, (s[0], s[2]), f32, "weight"), float(eps),
+            _ptr(h, s, T, "h", True), _ptr(y, s, T, "y", True), _ptr(q, s, torch.int8, "q", True),
+            _ptr(q_scale, s[:2], f32, "q_scale", True), _ptr(rstd, s[:2], f32, "rstd", True))
+    _here(x, weight, y, q, q_scale, residual, h, rstd)
+    _check(_lib.clt_rms_norm(_stream(), *s, *args))
+
+
+def clt_rms_norm_backward_workspace_bytes(L, B, d) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.clt_rms_norm_backward_workspace_bytes(L, B, d, C.byref(n)))
+    return n.value
+
+
+def clt_rms_norm_backward(h, weight, rstd, dy, dx, dweight=None, workspace=None, dh=None):
+    """Gradients of clt_rms_norm; dx may be dy or dh.  workspace: uint8, clt_rms_norm_backward_workspace_bytes, with dweight."""
+    dt, T = _storage(h, "h")
+    f32, s = torch.float32, tuple(h.shape)
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    args = (dt, _ptr(h, s, T, "h"), _ptr(weight, (s[0], s[2]), f32, "weight"), _ptr(rstd, s[:2], f32, "rstd"), _ptr(dy, s, T, "dy"),
+            _ptr(dh, s, T, "dh", True), _ptr(dx, s, T, "dx"), _ptr(dweight, (s[0], s[2]), f32, "dweight", True),
+            workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0)
+    _here(h, weight, rstd, dy, dx, dweight, workspace, dh)
+    _check(_lib.clt_rms_norm_backward(_stream(), *s, *args))
+
+
+ADAMW_BLOCK = 128
+
+
+class AdamWTensor:
+    """One tensor of clt_adamw_step: parameters p, gradient g (each float32 or bfloat16), moments m and v: float32, or uint8
+    with the block scales m_scale and v_scale (uint8, one per 128 elements); master: float32 copy of p.  Any shape,
+    contiguous; p, g, m, v and master have the same number of elements."""
+
+    def __init__(self, p, g, m, v, m_scale=None, v_scale=None, master=None, weight_decay=0.0):
+        n = p.numel()
+        eight = m.dtype == torch.uint8
+        types = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+        if p.dtype not in types or g.dtype not in types:
+            raise ValueError(f"p and g must be float32 or bfloat16, got {p.dtype} and {g.dtype}")
+        if eight != (m_scale is not None) or eight != (v_scale is not None):
+            raise ValueError("m_scale and v_scale belong to 8-bit (uint8) moments")
+        state = torch.uint8 if eight else torch.float32
+        flat = ((p, p.dtype, "p"), (g, g.dtype, "g"), (m, state, "m"), (v, state, "v"), (master, torch.float32, "master"))
+        for t, dt, name in flat:
+            _ptr(t, tuple(t.shape) if t is not None and t.numel() == n else (n,), dt, name, name == "master")
+        blocks = ((n + ADAMW_BLOCK - 1) // ADAMW_BLOCK,)
+        _ptr(m_scale, blocks, torch.uint8, "m_scale", True)
+        _ptr(v_scale, blocks, torch.uint8, "v_scale", True)
+        self.tensors = (p, g, m, v, m_scale, v_scale, master)      # kept alive
+        self.c = clt_adamw_tensor(*(None if t is None else t.data_ptr() for t in self.tensors), n, types[p.dtype], types[g.dtype],
+                                  8 if eight else 32, float(weight_decay))
+
+
+def _adamw_array(tensors):
+    return (clt_adamw_tensor * max(1, len(tensors)))(*(t.c for t in tensors))
+
+
+def clt_adamw_step(tensors, t, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
+    """One AdamW step over a list of AdamWTensor (include/clt.h)."""
+    AdamW(tensors, beta1, beta2, eps, seed).step(t, lr)
+
+
+class AdamW:
+    """AdamW over a list of AdamWTensor that stays the same from step to step (a training loop checks it once)."""
+
+    def __init__(self, tensors, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
+        self.tensors = list(tensors)
+        _here(*(x for t in self.tensors for x in t.tensors if x is not None))
+        self.device = torch.cuda.current_device() if self.tensors else None
+        self._array = _adamw_array(self.tensors)
+        self.scalars = (float(beta1), float(beta2), float(eps), int(seed))
+
+    @staticmethod
+    def moments(p, bits=32):
+        """Zero moments for a parameter: (m, v, m_scale, v_scale) of an AdamWTensor."""
+        if bits == 32:
+            return torch.zeros_like(p, dtype=torch.float32), torch.zeros_like(p, dtype=torch.float32), None, None
+        if bits != 8:
+            raise ValueError(f"moments are held in 32 or 8 bits, not {bits}")
+        z = lambda *s: torch.zeros(s, dtype=torch.uint8, device=p.device)
+        blocks = (p.numel() + ADAMW_BLOCK - 1) // ADAMW_BLOCK
+        return z(*p.shape), z(*p.shape), z(blocks), z(blocks)
+
+    def step(self, t, lr):
+        if self.device is not None and torch.cuda.current_device() != self.device:
+            raise ValueError(f"the tensors are on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
+        _check(_lib.clt_adamw_step(_stream(), len(self.tensors), self._array, int(t), float(lr), *self.scalars))
+
+
+def clt_mx4_bytes(L, rows, K):
+    """(bytes of the codes, bytes of the scales) of a packed 4-bit matrix [L][rows][K]."""
+    c, s = C.c_size_t(0), C.c_size_t(0)
+    _check(_lib.clt_mx4_bytes(L, rows, K, C.byref(c), C.byref(s)))
+    return c.value, s.value
+
+
+def mx4_empty(L, rows, K, device="cuda:0"):
+    """Room for a packed 4-bit matrix [L][rows][K]: (codes, scales), uint8."""
+    clt_mx4_bytes(L, rows, K)
+    rp, ks = (rows + 63) // 64, (K + 127) // 128
+    return (torch.empty((L, 4 * rp, ks, 1024), dtype=torch.uint8, device=device),
+            torch.empty((L, rp, ks, 256), dtype=torch.uint8, device=device))
+
+
+def _packed(codes, scales, L, rows, K, name):
+    rp, ks = (rows + 63) // 64, (K + 127) // 128
+    return (_ptr(codes, (L, 4 * rp, ks, 1024), torch.uint8, f"{name}codes"), _ptr(scales, (L, rp, ks, 256), torch.uint8, f"{name}scales"))
+
+
+def clt_mx4_quantise(a, codes, scales, a_scale=None, transposed=False):
+    """Packs a [L, rows, K] (float32, bfloat16, or int8 with a_scale [L, rows]; transposed: [L, K, rows]) into 4 bits."""
+    if a is not None and a.dtype == torch.int8:
+        if a.dim() != 3:
+            raise ValueError(f"a: expected a 3-dimensional tensor, got {tuple(a.shape)}")
+        dt, T, fmt = DTYPE_BF16, torch.int8, INPUT_INT8_ROWSCALE
+    else:
+        (dt, T), fmt = _storage(a, "a"), INPUT_NATIVE
+    s = tuple(a.shape)
+    L, rows, K = (s[0], s[2], s[1]) if transposed else s
+    args = (L, rows, K, dt, fmt, int(transposed), _ptr(a, s, T, "a"), _ptr(a_scale, (L, rows), torch.float32, "a_scale", True),
+            *_packed(codes, scales, L, rows, K, ""))
+    _here(a, a_scale, codes, scales)
+    _check(_lib.clt_mx4_quantise(_stream(), *args))
+
+
+def clt_mx4_dequantise(codes, scales, out):
+    """The values of a packed matrix into out [L, rows, K] float32 or bfloat16."""
+    dt, T = _storage(out, "out")
+    L, rows, K = out.shape
+    args = (L, rows, K, dt, *_packed(codes, scales, L, rows, K, ""), _ptr(out, (L, rows, K), T, "out"))
+    _here(codes, scales, out)
+    _check(_lib.clt_mx4_dequantise(_stream(), *args))
+
+
+def clt_mx4_product(a_codes, a_scales, b_codes, b_scales, out, K, bias=None, theta=None):
+    """out [L, M, N] = A B^T + bias of packed A [L][M][K] and B [L][N][K], with theta kept where above it, else 0."""
+    dt, T = _storage(out, "out")
+    L, M, N = out.shape
+    f32 = torch.float32
+    args = (L, M, N, int(K), *_packed(a_codes, a_scales, L, M, K, "a_"), *_packed(b_codes, b_scales, L, N, K, "b_"),
+            _ptr(bias, (L, N), f32, "bias", True), _ptr(theta, (L, N), f32, "theta", True), dt, _ptr(out, (L, M, N), T, "out"))
+    _here(a_codes, a_scales, b_codes, b_scales, out, bias, theta)
+    _check(_lib.clt_mx4_product(_stream(), *args))
+
+
 _VIEWS = {"norms": (0, torch.float32, lambda c: (c.L, c.F)), "d_yhat": (1, None, lambda c: (c.L, c.B, c.d)),
           "dpre": (2, None, lambda c: (c.L, c.B, c.F)), "G": (3, torch.float32, lambda c: (c.L, c.F)),
           "decode_switch": (4, torch.int32, lambda c: (5,))}
@@ -338,6 +526,7 @@ class CLTStep:
         if ws is None:
             ws = torch.empty(clt_workspace_bytes(self.cfg), dtype=torch.uint8, device=self.device)
         self.H = clt_init(self.cfg, ws)
+        self.adam = (beta1, beta2, adam_eps)
         T = self.H.T
         P = L * (L + 1) // 2
         e = lambda *s, dtype=T: torch.empty(s, dtype=dtype, device=self.device)
@@ -376,12 +565,28 @@ class CLTStep:
     def backward_adam_step(self, x, params, m, v, t, lr, master=None, x_scale=None):
         clt_backward_adam_step(self.H, x, self.z, self.act_class, t, lr, params, self.grads, m, v, master, x_scale)
 
+    def adamw(self, params, bits=8, master=None, weight_decay=0.0, seed=0):
+        """An AdamW over this step's gradients for train_step: moments of the matrices in 8 or 32 bits, beginning at zero, those
+        of the vectors in 32; weight decay and master copies for the matrices.  Needs matrix_grads."""
+        if "W_dec" not in self.grads:
+            raise ValueError("adamw needs the matrices' gradients (matrix_grads=True)")
+        tensors = []
+        for k, g in self.grads.items():
+            matrix = k in ("W_enc", "W_dec")
+            tensors.append(AdamWTensor(params[k], g, *AdamW.moments(params[k], bits if matrix else 32), (master or {}).get(k) if matrix else None,
+                                       weight_decay if matrix else 0.0))
+        return AdamW(tensors, *self.adam, seed)
+
     def train_step(self, x, y, params, m, v, t, lr, lambda0, master=None, x_scale=None, y_scale=None, fused=True,
-                   lambda1=0.0):
-        """forward, loss, backward and Adam; `fused` runs Adam inside the weight-gradient GEMMs."""
+                   lambda1=0.0, optimiser=None):
+        """forward, loss, backward and Adam; `fused` runs Adam inside the weight-gradient GEMMs.  With an optimiser (see adamw) its
+        step takes Adam's place: m, v, master and fused are not used."""
         self.forward(x, params, x_scale)
         self.loss(y, lambda0, y_scale, False, lambda1, params)
-        if fused:
+        if optimiser is not None:
+            self.backward(x, params, x_scale)
+            optimiser.step(t, lr)
+        elif fused:
             self.backward_adam_step(x, params, m, v, t, lr, master, x_scale)
         else:
             self.backward(x, params, x_scale)

@@ -798,4 +798,180 @@ int clt_adam_step(clt_handle* h, void* stream, int64_t t, float lr, const clt_te
   return CLT_OK;
 }
 
+
+// ---- around the training step: no handle, errors on the calling thread --------------------------------------------
+#define FAIL(code, ...)                 \
+  do {                                  \
+    set_err(g_err, __VA_ARGS__);        \
+    return code;                        \
+  } while (0)
+#define NEED(ptr)                                                                              \
+  do {                                                                                         \
+    if (!(ptr)) FAIL(CLT_ERR_INVALID_ARG, "%s: argument %s is NULL", __func__, #ptr);          \
+    if (misaligned(ptr)) FAIL(CLT_ERR_ALIGN, "%s: argument %s is not 16-byte aligned", __func__, #ptr); \
+  } while (0)
+#define MAY(ptr)                                                                               \
+  do {                                                                                         \
+    if ((ptr) && misaligned(ptr)) FAIL(CLT_ERR_ALIGN, "%s: argument %s is not 16-byte aligned", __func__, #ptr); \
+  } while (0)
+#define LAUNCH(expr)                                                                           \
+  do {                                                                                         \
+    const hipError_t e__ = (expr);                                                             \
+    if (e__ != hipSuccess) {                                                                   \
+      (void)hipGetLastError();                                                                 \
+      FAIL(CLT_ERR_HIP, "%s: launch failed: %s", __func__, hipGetErrorString(e__));            \
+    }                                                                                          \
+  } while (0)
+
+static int check_rows(const char* who, int32_t L, int32_t B, int32_t d) {
+  if (L < 1 || L > 128 || B < 1 || d < 8 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 31)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^31, d a positive multiple of 8)", who, L, B, d);
+  return CLT_OK;
+}
+
+int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
+                 const float* weight, float eps, void* h, void* y, int8_t* q, float* q_scale, float* rstd) {
+  const int rc = check_rows(__func__, L, B, d);
+  if (rc != CLT_OK) return rc;
+  if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: bad dtype %d", dtype);
+  if (!(eps > 0.f)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: eps must be > 0");
+  NEED(x); NEED(weight);
+  MAY(residual); MAY(h); MAY(y); MAY(q); MAY(q_scale); MAY(rstd);
+  if ((residual != nullptr) != (h != nullptr)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: residual and h go together");
+  if ((q != nullptr) != (q_scale != nullptr)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: q and q_scale go together");
+  if (!y && !q) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: neither y nor q is given");
+  LAUNCH(launch_rms_norm(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, B, d,
+                         RmsNormArgs{x, residual, weight, eps, h, y, q, q_scale, rstd}));
+  return CLT_OK;
+}
+
+int clt_rms_norm_backward_workspace_bytes(int32_t L, int32_t B, int32_t d, size_t* bytes) {
+  if (!bytes) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm_backward_workspace_bytes: bytes is NULL");
+  const int rc = check_rows(__func__, L, B, d);
+  if (rc != CLT_OK) return rc;
+  *bytes = rms_norm_backward_floats(L, B, d) * sizeof(float);
+  return CLT_OK;
+}
+
+int clt_rms_norm_backward(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* h, const float* weight,
+                          const float* rstd, const void* dy, const void* dh, void* dx, float* dweight, void* workspace,
+                          size_t workspace_bytes) {
+  const int rc = check_rows(__func__, L, B, d);
+  if (rc != CLT_OK) return rc;
+  if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm_backward: bad dtype %d", dtype);
+  NEED(h); NEED(weight); NEED(rstd); NEED(dy); NEED(dx);
+  MAY(dh); MAY(dweight);
+  if (dweight) {
+    const size_t need = rms_norm_backward_floats(L, B, d) * sizeof(float);
+    if (!workspace || misaligned(workspace) || workspace_bytes < need)
+      FAIL(CLT_ERR_WORKSPACE, "clt_rms_norm_backward: workspace must be non-NULL, 16-byte aligned and at least %zu bytes (got %zu)", need, workspace_bytes);
+  }
+  LAUNCH(launch_rms_norm_backward(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, B, d,
+                                  RmsNormBackwardArgs{h, weight, rstd, dy, dh, dx, dweight, static_cast<float*>(workspace)}));
+  return CLT_OK;
+}
+
+int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tensors, int64_t t, double lr, double beta1,
+                   double beta2, double eps, uint64_t seed) {
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors)) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad list of tensors");
+  if (t < 1) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: step count t must be >= 1");
+  if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f))
+    FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: need lr>=0, 0<=beta<1, eps>0");
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const clt_adamw_tensor& q = tensors[i];
+    if (q.n < 0 || q.n > (int64_t)1 << 40) FAIL(CLT_ERR_SHAPE, "clt_adamw_step: tensor %d has n=%lld (need 0<=n<=2^40)", i, (long long)q.n);
+    if ((q.dtype != CLT_DTYPE_F32 && q.dtype != CLT_DTYPE_BF16) || (q.grad_dtype != CLT_DTYPE_F32 && q.grad_dtype != CLT_DTYPE_BF16) ||
+        (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f))
+      FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: bad dtype, grad_dtype, state_bits or weight_decay", i);
+    if (q.n == 0) continue;
+    if (!q.p || !q.g || !q.m || !q.v) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: p, g, m and v are required", i);
+    if ((q.state_bits == 8) != (q.m_scale != nullptr) || (q.state_bits == 8) != (q.v_scale != nullptr))
+      FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: m_scale and v_scale belong to 8-bit moments", i);
+    if (misaligned(q.p) || misaligned(q.g) || misaligned(q.m) || misaligned(q.v) || misaligned(q.m_scale) || misaligned(q.v_scale) || misaligned(q.master))
+      FAIL(CLT_ERR_ALIGN, "clt_adamw_step: tensor %d: a pointer is not 16-byte aligned", i);
+  }
+  const double bc1 = 1.0 - pow(beta1, (double)t), bc2 = 1.0 - pow(beta2, (double)t);
+  AdamWList list{};
+  list.a = AdamScalars{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 / bc2), (float)(-lr / bc1), (float)eps};
+  const uint32_t key_t = adamw_mix((uint32_t)((uint64_t)t >> 32)) ^ (uint32_t)t;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const clt_adamw_tensor& q = tensors[i];
+    const uint32_t chunks = (uint32_t)((q.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK);      // at most 2^29
+    if (list.count == ADAMW_TENSORS || (uint64_t)list.chunks + chunks >= (uint64_t)1 << 31) {
+      LAUNCH(launch_adamw(static_cast<hipStream_t>(stream), list));
+      list.count = 0; list.chunks = 0;
+    }
+    if (chunks == 0) continue;
+    const uint32_t key = adamw_mix((uint32_t)seed ^ adamw_mix((uint32_t)(seed >> 32) ^ adamw_mix(key_t ^ adamw_mix((uint32_t)i + 0x243F6A88u))));
+    list.t[list.count++] = AdamWTensor{q.p, q.g, q.m, q.v, q.m_scale, q.v_scale, q.master, q.n, list.chunks, key,
+                                       (float)(1.0 - lr * (double)q.weight_decay), (uint8_t)(q.dtype == CLT_DTYPE_BF16),
+                                       (uint8_t)(q.grad_dtype == CLT_DTYPE_BF16), (uint8_t)(q.state_bits == 8), 0};
+    list.chunks += chunks;
+  }
+  if (list.count) LAUNCH(launch_adamw(static_cast<hipStream_t>(stream), list));
+  return CLT_OK;
+}
+
+// (the sizes that the kernels' 32-bit block counts and grids hold)
+static int check_packed(const char* who, int32_t L, int32_t rows, int32_t K) {
+  if (L < 1 || L > 65535 || rows < 1 || rows > 1 << 20 || K < 8 || (K % 8) || (int64_t)rows * mx4_steps(K) >= (int64_t)1 << 28)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d rows=%d K=%d (need 1<=L<=65535, 1<=rows<=2^20, K a positive multiple of 8, rows*ceil(K/128)<2^28)",
+         who, L, rows, K);
+  return CLT_OK;
+}
+
+int clt_mx4_bytes(int32_t L, int32_t rows, int32_t K, size_t* codes_bytes, size_t* scales_bytes) {
+  if (!codes_bytes || !scales_bytes) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_bytes: a result pointer is NULL");
+  const int rc = check_packed(__func__, L, rows, K);
+  if (rc != CLT_OK) return rc;
+  const size_t tiles = (size_t)L * mx4_panels(rows) * mx4_steps(K);
+  *codes_bytes = tiles * 4096;
+  *scales_bytes = tiles * 256;
+  return CLT_OK;
+}
+
+int clt_mx4_quantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t dtype, int32_t input_format, int32_t transposed,
+                     const void* a, const float* a_scale, void* codes, void* scales) {
+  const int rc = check_packed(__func__, L, rows, K);
+  if (rc != CLT_OK) return rc;
+  const bool int8 = input_format == CLT_INPUT_INT8_ROWSCALE;
+  if ((dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) || (input_format != CLT_INPUT_NATIVE && !int8) || (int8 && dtype != CLT_DTYPE_BF16) ||
+      (transposed != 0 && transposed != 1))
+    FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_quantise: bad dtype %d / input_format %d / transposed %d", dtype, input_format, transposed);
+  if (transposed && int8) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_quantise: int8 rows have their scales along the rows, not transposed");
+  if (transposed && (rows % 8)) FAIL(CLT_ERR_SHAPE, "clt_mx4_quantise: transposed needs rows (%d) a multiple of 8", rows);
+  NEED(a); NEED(codes); NEED(scales);
+  if (int8) NEED(a_scale);
+  else if (a_scale) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_quantise: a_scale given but input_format is native");
+  LAUNCH(launch_mx4_quantise(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, int8, transposed != 0, L, rows, K, a, a_scale,
+                             static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales)));
+  return CLT_OK;
+}
+
+int clt_mx4_dequantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t dtype, const void* codes, const void* scales,
+                       void* out) {
+  const int rc = check_packed(__func__, L, rows, K);
+  if (rc != CLT_OK) return rc;
+  if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_dequantise: bad dtype %d", dtype);
+  NEED(codes); NEED(scales); NEED(out);
+  LAUNCH(launch_mx4_dequantise(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, rows, K,
+                               Mx4{static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales)}, out));
+  return CLT_OK;
+}
+
+int clt_mx4_product(void* stream, int32_t L, int32_t M, int32_t N, int32_t K, const void* a_codes, const void* a_scales,
+                    const void* b_codes, const void* b_scales, const float* bias, const float* theta, int32_t dtype, void* out) {
+  int rc = check_packed(__func__, L, M, K);
+  if (rc == CLT_OK) rc = check_packed(__func__, L, N, K);
+  if (rc != CLT_OK) return rc;
+  if (N % 8) FAIL(CLT_ERR_SHAPE, "clt_mx4_product: N=%d must be a multiple of 8", N);
+  if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_product: bad dtype %d", dtype);
+  NEED(a_codes); NEED(a_scales); NEED(b_codes); NEED(b_scales); NEED(out);
+  MAY(bias); MAY(theta);
+  LAUNCH(launch_mx4_product(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, M, N, K,
+                            Mx4{static_cast<const uint8_t*>(a_codes), static_cast<const uint8_t*>(a_scales)},
+                            Mx4{static_cast<const uint8_t*>(b_codes), static_cast<const uint8_t*>(b_scales)}, bias, theta, out));
+  return CLT_OK;
+}
+
 }  // extern "C"

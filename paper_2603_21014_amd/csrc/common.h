@@ -410,4 +410,39 @@ hipError_t launch_dz_from_partials(hipStream_t s, bool bf16, Dims D, FeatureList
 hipError_t launch_sparse_dwdec(hipStream_t s, bool bf16, Dims D, FeatureLists fl, const DWdecArgs& a,
                                const int32_t* flags);
 
+// ---- RMS norm (kernels_rms_norm.hip), see clt_rms_norm -------------------------------------------------------------
+struct RmsNormArgs {
+  const void* x; const void* residual; const float* weight; float eps; void* h; void* y; int8_t* q; float* q_scale; float* rstd;
+};
+hipError_t launch_rms_norm(hipStream_t s, bool bf16, int L, int B, int d, const RmsNormArgs& a);
+struct RmsNormBackwardArgs {
+  const void* h; const float* weight; const float* rstd; const void* dy; const void* dh; void* dx; float* dweight; float* part;
+};
+size_t rms_norm_backward_floats(int L, int B, int d);      // room for the partial sums of dweight
+hipError_t launch_rms_norm_backward(hipStream_t s, bool bf16, int L, int B, int d, const RmsNormBackwardArgs& a);
+
+// ---- AdamW over many tensors (kernels_adamw.hip), see clt_adamw_step ----------------------------------------------
+constexpr int ADAMW_TENSORS = 32;      // of one launch: their descriptions are kernel arguments (2.6 KB)
+constexpr int ADAMW_CHUNK = 2048;      // elements of a workgroup
+struct AdamWTensor {
+  void* p; const void* g; void* m; void* v; uint8_t* m_scale; uint8_t* v_scale; float* master;
+  int64_t n; uint32_t chunk0;          // first chunk in the launch
+  uint32_t key;                        // of the random bits
+  float keep;                          // 1 - lr * weight_decay
+  uint8_t bf16, grad_bf16, state8, pad;
+};
+struct AdamWList { int count; uint32_t chunks; AdamScalars a; AdamWTensor t[ADAMW_TENSORS]; };
+uint32_t adamw_mix(uint32_t x);
+hipError_t launch_adamw(hipStream_t s, const AdamWList& q);
+
+// ---- 4-bit microscaled floating point (kernels_mx4.hip), see clt_mx4_quantise -------------------------------------
+inline int mx4_steps(int K) { return (K + 127) / 128; }
+inline int mx4_panels(int rows) { return (rows + 63) / 64; }
+struct Mx4 { const uint8_t* codes; const uint8_t* scales; };
+hipError_t launch_mx4_quantise(hipStream_t s, bool bf16, bool int8, bool transposed, int L, int rows, int K, const void* a,
+                               const float* a_scale, uint8_t* codes, uint8_t* scales);
+hipError_t launch_mx4_dequantise(hipStream_t s, bool bf16, int L, int rows, int K, Mx4 a, void* out);
+hipError_t launch_mx4_product(hipStream_t s, bool bf16, int L, int M, int N, int K, Mx4 a, Mx4 b, const float* bias, const float* theta,
+                              void* out);
+
 }  // namespace clt

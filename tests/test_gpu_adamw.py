@@ -1,0 +1,222 @@
+"""AdamW over many tensors, moments in 32 and in 8 bits, against the oracle: moments bit for bit, parameters within rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as R
+from operators_testlib import DEV, HALF, T, U, Guarded, normal, np32, np64, replayed
+
+pytestmark = pytest.mark.gpu
+LR, B1, B2, EPS, SEED = 1e-3, 0.9, 0.999, 1e-8, 0x123456789ABCDEF
+
+
+class Case:
+    """One tensor: host values (float32 arrays) and its device side between guards."""
+
+    def __init__(self, K, n, dtype="bf16", grad="bf16", bits=8, master=False, decay=0.01, seed=0, started=True):
+        self.n, self.dtype, self.grad, self.bits, self.master, self.decay = n, dtype, grad, bits, master, decay
+        self.p = np32(normal(seed + 1, n).to(T[dtype]))
+        self.w = np32(normal(seed + 5, n)) if master else self.p
+        self.m, self.v = np.zeros(n, np.float32), np.zeros(n, np.float32)
+        self.ms = self.vs = None
+        if bits == 8:
+            blocks = -(-n // 128)
+            self.m, self.v = np.zeros(n, np.uint8), np.zeros(n, np.uint8)
+            self.ms, self.vs = np.zeros(blocks, np.uint8), np.zeros(blocks, np.uint8)
+            if started:
+                rng = np.random.default_rng(seed)
+                self.m, self.v = rng.integers(0, 256, n).astype(np.uint8), rng.integers(0, 0x7C, n).astype(np.uint8)
+                self.m[(self.m & 0x7F) == 0x7F] = 0x12
+                self.ms, self.vs = rng.integers(100, 110, blocks).astype(np.uint8), rng.integers(85, 95, blocks).astype(np.uint8)
+        elif started:
+            self.m, self.v = np32(1e-2 * normal(seed + 2, n)), np32(1e-4 * normal(seed + 3, n).square())
+        dev = lambda a, dt: Guarded((n,), dt, torch.from_numpy(a))
+        st = torch.uint8 if bits == 8 else torch.float32
+        self.dp, self.dg = dev(self.p, T[dtype]), Guarded((n,), T[grad])
+        self.dm, self.dv = dev(self.m, st), dev(self.v, st)
+        self.dw = dev(self.w, torch.float32) if master else None
+        self.dms = Guarded(self.ms.shape, torch.uint8, torch.from_numpy(self.ms)) if bits == 8 else None
+        self.dvs = Guarded(self.vs.shape, torch.uint8, torch.from_numpy(self.vs)) if bits == 8 else None
+        o = lambda g: g.t if g else None
+        self.c = K.AdamWTensor(self.dp.t, self.dg.t, self.dm.t, self.dv.t, o(self.dms), o(self.dvs), o(self.dw), decay)
+
+    def gradient(self, seed, size=1e-2):
+        # features of very different sizes, and some exact zeros
+        g = size * normal(seed, self.n) * torch.exp(2 * normal(seed + 1, (self.n + 63) // 64).repeat_interleave(64)[:self.n])
+        g[normal(seed + 2, self.n) > 1.5] = 0.0
+        self.g = np32(g.to(T[self.grad]))
+        self.dg.t.copy_(torch.from_numpy(self.g))
+
+    def check(self, t, index, lr=LR):
+        o = R.adamw(self.w, self.g, self.m, self.v, t, lr, B1, B2, EPS, float(np.float32(self.decay)), self.ms, self.vs, SEED, index)
+        got_m, got_v = self.dm.t.cpu().numpy(), self.dv.t.cpu().numpy()
+        if self.bits == 8:
+            assert np.array_equal(self.dms.t.cpu().numpy(), o["m_scale"]) and np.array_equal(self.dvs.t.cpu().numpy(), o["v_scale"])
+            self.ms, self.vs = o["m_scale"], o["v_scale"]
+        assert np.array_equal(got_m, o["m"]) and np.array_equal(got_v, o["v"])
+        self.m, self.v = o["m"], o["v"]
+        # update: square root, reciprocal (one unit each), four products; parameter: product with 1 - lr decay and the addition
+        step = np.abs(np.asarray(self.w, np.float64) * (1 - lr * float(np.float32(self.decay))) - o["p"])
+        bound = step * 16 * U + np.abs(self.w) * 3 * U + 1e-38
+        got = np64(self.dp.t)
+        if self.master:
+            assert np.all(np.abs(np64(self.dw.t) - o["p"]) <= bound)
+            assert torch.equal(self.dp.t, self.dw.t.to(T[self.dtype]))
+            self.w = np32(self.dw.t)
+        else:
+            assert np.all(np.abs(got - o["p"]) <= bound * 2 + HALF[self.dtype] * np.abs(o["p"]) * 1.01)
+            self.w = np32(self.dp.t)
+        for g in (self.dp, self.dg, self.dm, self.dv, self.dw, self.dms, self.dvs):
+            if g:
+                g.check()
+
+
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 127, 128, 129, 1000, 2047, 2048, 2049, 4096 + 120, 300001])
+@pytest.mark.parametrize("dtype,grad,bits,master", [("bf16", "bf16", 8, False), ("bf16", "f32", 8, True), ("f32", "f32", 8, False), ("f32", "bf16", 32, False),
+                                                    ("bf16", "bf16", 32, True), ("f32", "f32", 32, False), ("bf16", "f32", 32, False), ("f32", "f32", 8, True)])
+def test_one_tensor(n, dtype, grad, bits, master):
+    from paper_2603_21014_amd import binding as K
+    c = Case(K, n, dtype, grad, bits, master, seed=n)
+    opt = K.AdamW([c.c], B1, B2, EPS, SEED)
+    for t in (7, 8):
+        c.gradient(100 * t + n)
+        opt.step(t, LR)
+        torch.cuda.synchronize()
+        c.check(t, 0)
+
+
+def test_many_tensors_of_all_kinds_in_one_call():
+    """70 tensors (three launches), empty ones among them, sizes from 1 to some 10,000, every combination of types."""
+    from paper_2603_21014_amd import binding as K
+    rng = np.random.default_rng(2)
+    cases = []
+    for i in range(70):
+        n = 0 if i % 11 == 5 else int(np.exp(rng.uniform(0, 10)))
+        dtype, grad = ("bf16", "f32")[i & 1], ("bf16", "f32")[(i >> 1) & 1]
+        cases.append(Case(K, n, dtype, grad, (8, 32)[(i >> 2) & 1], bool((i >> 3) & 1), 0.05 * (i % 3), seed=i, started=i % 5 != 0))
+    opt = K.AdamW([c.c for c in cases], B1, B2, EPS, SEED)
+    for t in (1, 2):
+        for i, c in enumerate(cases):
+            c.gradient(1000 * t + 10 * i)
+        opt.step(t, LR)
+        torch.cuda.synchronize()
+        for i, c in enumerate(cases):
+            if c.n:
+                c.check(t, i)
+
+
+def test_agrees_with_the_existing_adam_step_without_decay():
+    from paper_2603_21014_amd import binding as K
+    L, d, F, B = 2, 64, 136, 8
+    step = K.CLTStep(L, d, F, B, dtype="bf16", device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    params = {k: torch.randn(s.shape, generator=g, device=DEV).to(s.dtype) for k, s in step.grads.items()}
+    for k in step.grads:
+        step.grads[k].copy_(1e-2 * torch.randn(step.grads[k].shape, generator=g, device=DEV))
+    mine = {k: p.clone() for k, p in params.items()}
+    m, v = ({k: torch.zeros_like(p, dtype=torch.float32) for k, p in params.items()} for _ in range(2))
+    m2, v2 = ({k: torch.zeros_like(p, dtype=torch.float32) for k, p in params.items()} for _ in range(2))
+    opt = K.AdamW([K.AdamWTensor(mine[k], step.grads[k], m2[k], v2[k]) for k in params])
+    for t in (1, 2, 3):
+        step.adam_step(t, 1e-3, params, m, v)
+        opt.step(t, 1e-3)
+    for k in params:      # (the existing step forms 1 - beta from the rounded betas: 2e-7 and 2e-5 of the moments)
+        half = HALF["bf16" if params[k].dtype == torch.bfloat16 else "f32"]
+        assert np.allclose(np64(m[k]), np64(m2[k]), rtol=1e-6, atol=1e-12) and np.allclose(np64(v[k]), np64(v2[k]), rtol=4e-5, atol=1e-16)
+        assert np.all(np.abs(np64(params[k]) - np64(mine[k])) <= 3 * (1e-3 * 1e-4 + 2 * half * np.abs(np64(mine[k]))))
+
+
+def test_broken_gradients_show_in_their_block_only():
+    from paper_2603_21014_amd import binding as K
+    for bad in (float("nan"), float("inf"), -float("inf"), 3e38):
+        c = Case(K, 500, "f32", "f32", 8, seed=4)
+        c.gradient(5)
+        c.dg.t[130] = bad
+        c.g[130] = bad
+        opt = K.AdamW([c.c], B1, B2, EPS, SEED)
+        opt.step(3, LR)
+        vs, ms = c.dvs.t.cpu(), c.dms.t.cpu()
+        assert vs[1] == 255 and (vs[[0, 2, 3]] < 255).all() and (ms[[0, 2, 3]] < 255).all()
+        assert ms[1] == (255 if abs(bad) > 3.2e38 or bad != bad else ms[1])
+        p = c.dp.t.cpu()
+        if bad != 3e38:      # (that one's own update is finite: lr m / sqrt(inf) = 0)
+            assert torch.isnan(p[130])
+        assert torch.isfinite(p[:128]).all() and torch.isfinite(p[256:]).all()
+        opt.step(4, LR)      # the block's state is gone, and says so
+        p = c.dp.t.cpu()
+        assert torch.isnan(p[128:256]).all() and torch.isfinite(p[:128]).all() and torch.isfinite(p[256:]).all()
+
+
+def test_small_second_moments_never_round_to_zero():
+    """One large element in a block of tiny ones: their second moments would be lost below the block's range, and a first
+    moment over a root of zero is an update of m / eps."""
+    from paper_2603_21014_amd import binding as K
+    c = Case(K, 128, "f32", "f32", 8, seed=6, started=False)
+    c.gradient(7)
+    c.dg.t.fill_(1e-7)
+    c.dg.t[5] = 1.0
+    c.dg.t[6] = 0.0
+    c.g = c.dg.t.cpu().numpy()
+    opt = K.AdamW([c.c], B1, B2, EPS, SEED)
+    for t in (1, 2, 3):
+        before = c.dp.t.clone()
+        opt.step(t, LR)
+        torch.cuda.synchronize()
+        c.check(t, 0)
+        assert (c.dp.t - before).abs().max() < 20 * LR
+    v = c.dv.t.cpu()
+    assert (v[torch.arange(128) != 6] > 0).all() and v[6] == 0
+
+
+def test_repeatable_and_seeded():
+    from paper_2603_21014_amd import binding as K
+    states = []
+    for seed in (SEED, SEED, SEED + 1):
+        c = Case(K, 5000, "bf16", "bf16", 8, seed=8)
+        c.gradient(9)
+        K.clt_adamw_step([c.c], 11, LR, B1, B2, EPS, seed)
+        states.append((c.dm.t.clone(), c.dv.t.clone(), c.dp.t.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(states[0], states[1]))
+    assert not torch.equal(states[0][0], states[2][0]) and torch.equal(states[0][2], states[2][2])
+
+
+def test_streams_and_graphs():
+    """A captured step is the same step at every replay (t, lr and seed are those of the capture)."""
+    from paper_2603_21014_amd import binding as K
+    a, b = Case(K, 70000, "bf16", "bf16", 8, seed=12), Case(K, 70000, "bf16", "bf16", 8, seed=12)
+    a.gradient(13)
+    b.gradient(13)
+    oa, ob = K.AdamW([a.c], B1, B2, EPS, SEED), K.AdamW([b.c], B1, B2, EPS, SEED)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        oa.step(5, LR)
+    s.synchronize()
+    ob.step(5, LR)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        oa.step(6, LR)
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        ob.step(6, LR)
+        torch.cuda.synchronize()
+        for x, y in ((a.dp, b.dp), (a.dm, b.dm), (a.dv, b.dv), (a.dms, b.dms), (a.dvs, b.dvs)):
+            assert torch.equal(x.t, y.t)
+
+
+def test_misaligned_and_foreign_tensors_are_refused():
+    from paper_2603_21014_amd import binding as K
+    x = torch.zeros(130, device=DEV)
+    with pytest.raises(K.CLTError) as e:
+        K.clt_adamw_step([K.AdamWTensor(x[1:129], x[:128].clone(), x[:128].clone(), x[:128].clone())], 1, LR)
+    assert e.value.code == -3
+    with pytest.raises(ValueError):
+        K.AdamWTensor(x, x, x[:100], x)
+    with pytest.raises(ValueError):
+        K.AdamWTensor(x[::2], x[::2].contiguous(), x[:65], x[:65])
+    with pytest.raises(ValueError):
+        K.AdamWTensor(x, x, x.to(torch.uint8), x.to(torch.uint8), x[:1].to(torch.uint8), x[:1].to(torch.uint8))
+    torch.cuda.synchronize()
+    assert not x.any()
