@@ -914,8 +914,8 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
 
 // (the sizes that the kernels' 32-bit block counts and grids hold)
 static int check_packed(const char* who, int32_t L, int32_t rows, int32_t K) {
-  if (L < 1 || L > 65535 || rows < 1 || rows > 1 << 20 || K < 8 || (K % 8) || (int64_t)rows * mx4_steps(K) >= (int64_t)1 << 28)
-    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d rows=%d K=%d (need 1<=L<=65535, 1<=rows<=2^20, K a positive multiple of 8, rows*ceil(K/128)<2^28)",
+  if (L < 1 || L > 65535 || rows < 1 || rows > 1 << 20 || K < 8 || K > 1 << 24 || (K % 8) || (int64_t)rows * mx4_steps(K) >= (int64_t)1 << 28)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d rows=%d K=%d (need 1<=L<=65535, 1<=rows<=2^20, K<=2^24 a positive multiple of 8, rows*ceil(K/128)<2^28)",
          who, L, rows, K);
   return CLT_OK;
 }
@@ -965,6 +965,7 @@ int clt_mx4_product(void* stream, int32_t L, int32_t M, int32_t N, int32_t K, co
   if (rc == CLT_OK) rc = check_packed(__func__, L, N, K);
   if (rc != CLT_OK) return rc;
   if (N % 8) FAIL(CLT_ERR_SHAPE, "clt_mx4_product: N=%d must be a multiple of 8", N);
+  if ((double)L * M * N >= 1e13) FAIL(CLT_ERR_SHAPE, "clt_mx4_product: L=%d M=%d N=%d: too many results", L, M, N);
   if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_product: bad dtype %d", dtype);
   NEED(a_codes); NEED(a_scales); NEED(b_codes); NEED(b_scales); NEED(out);
   MAY(bias); MAY(theta);

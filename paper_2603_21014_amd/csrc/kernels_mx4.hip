@@ -2,6 +2,8 @@
 // (clt_mx4_quantise, clt_mx4_dequantise, clt_mx4_product; the packed layout is described in include/clt.h).
 #include "common.h"
 
+#include <type_traits>
+
 namespace clt {
 namespace {
 
@@ -173,192 +175,316 @@ __global__ __launch_bounds__(256) void mx4_dequantise_kernel(int rows, int K, in
 //
 // v_mfma_scale_f32_16x16x128: a lane's operand is the 32 elements (16 bytes) of one block, row lane % 16, block lane / 16,
 // with the block's scale in one byte of a register that the instruction selects: what a packed tile of 16 rows holds at byte
-// 16 * lane.  The rows of B (features) are the instruction's first operand, those of A (tokens) its second, so a lane's
-// four results are four features of one token.  The sixteen rows that make up the j-th of a panel's four operands are free;
-// with rows 16 a + 4 j + b (a, b = 0..3) at lane 4 a + b, a lane ends up with sixteen consecutive features of its token:
-// 32 bytes of bf16 to store, and the four lanes of a token a whole 128-byte line.  The price are four byte loads of scales for a
-// panel's step instead of one dword.
+// 16 * lane, and what a panel's step holds of scales at byte 4 * lane.  The rows of B (features) are the instruction's first
+// operand, those of A (tokens) its second, so a lane's four results are four consecutive features of one token.
 
-// B operands of one panel (64 rows) and step
-struct PanelFrag { u32x4 c[4]; uint32_t s[4]; };
-struct PanelPtr {
-  const uint8_t* codes; const uint8_t* scales;
-  __device__ __forceinline__ PanelPtr(Mx4 b, size_t panel, int KS, int lane) {
-    const int kb = lane >> 4, a = (lane >> 2) & 3, r = lane & 3;
-    codes = b.codes + (((panel * 4 + a) * KS) << 10) + ((kb * 16 + r) << 4);
-    scales = b.scales + ((panel * KS) << 8) + ((kb * 16 + r) << 2) + a;
+// Loads of 16 or 4 bytes per lane, consecutive lanes, from `offset` bytes on: through buffer descriptors, which keep everything but
+// the lane's own offset (one register for all loads) in scalar registers.  A panel of K <= 2^24 is at most 2^29 bytes.
+struct Source {
+  __amdgpu_buffer_rsrc_t d;
+  __device__ __forceinline__ Source(const uint8_t* base) : d(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, 0x7fffffff, 0x00027000)) {}
+  __device__ __forceinline__ u32x4 lanes16(uint32_t lane, uint32_t offset) const {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(d, (int)(lane * 16), (int)offset, 0));
   }
-  __device__ __forceinline__ void load(PanelFrag& f, int ks) const {
-    const uint8_t *c = codes + ((size_t)ks << 10), *s = scales + ((size_t)ks << 8);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f.c[j] = *reinterpret_cast<const u32x4*>(c + 64 * j);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f.s[j] = s[16 * j];
+  __device__ __forceinline__ uint32_t lanes4(uint32_t lane, uint32_t offset) const {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(d, (int)(lane * 4), (int)offset, 0));
   }
 };
 
-template <int OP> __device__ __forceinline__ f32x4 mfma(u32x4 b, uint32_t bs, u32x4 a, uint32_t as, f32x4 c) {
+// Operands of one panel (64 rows) and step
+struct PanelFrag { u32x4 c[4]; uint32_t s; };
+struct Panel {
+  Source codes, scales; int KS;
+  __device__ __forceinline__ Panel(Mx4 b, size_t panel, int KS) : codes(b.codes + ((panel * 4 * KS) << 10)), scales(b.scales + ((panel * KS) << 8)), KS(KS) {}
+  __device__ __forceinline__ u32x4 tile(int j, int ks, uint32_t lane) const { return codes.lanes16(lane, (uint32_t)(j * KS + ks) << 10); }
+  __device__ __forceinline__ uint32_t scale(int ks, uint32_t lane) const { return scales.lanes4(lane, (uint32_t)ks << 8); }
+};
+
+template <int OB, int OA> __device__ __forceinline__ f32x4 mfma(u32x4 b, uint32_t bs, u32x4 a, uint32_t as, f32x4 c) {
   const i32x8 A = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, B = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B, A, c, 4, 4, 0, (int)bs, OP, (int)as);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B, A, c, 4, 4, OB, (int)bs, OA, (int)as);
 }
-// tile i of a 64-row panel of A has its scales in byte i
-__device__ __forceinline__ f32x4 mfma(int i, u32x4 b, uint32_t bs, u32x4 a, uint32_t as, f32x4 c) {
+// one tile of tokens, whose scales are in byte i of their panel's, by the four tiles of a panel of features
+template <int I> __device__ __forceinline__ void mfma4(const PanelFrag& b, u32x4 a, uint32_t as, f32x4 (&c)[4]) {
+  c[0] = mfma<0, I>(b.c[0], b.s, a, as, c[0]);
+  c[1] = mfma<1, I>(b.c[1], b.s, a, as, c[1]);
+  c[2] = mfma<2, I>(b.c[2], b.s, a, as, c[2]);
+  c[3] = mfma<3, I>(b.c[3], b.s, a, as, c[3]);
+}
+__device__ __forceinline__ void mfma4(int i, const PanelFrag& b, u32x4 a, uint32_t as, f32x4 (&c)[4]) {
   switch (i & 3) {
-    case 0: return mfma<0>(b, bs, a, as, c);
-    case 1: return mfma<1>(b, bs, a, as, c);
-    case 2: return mfma<2>(b, bs, a, as, c);
-    default: return mfma<3>(b, bs, a, as, c);
+    case 0: mfma4<0>(b, a, as, c); break;
+    case 1: mfma4<1>(b, a, as, c); break;
+    case 2: mfma4<2>(b, a, as, c); break;
+    default: mfma4<3>(b, a, as, c);
   }
 }
 
-// Sixteen consecutive features, n of them (0, 8 or 16, or less than 0) inside the matrix
-__device__ __forceinline__ void store_features(bf16_t* o, const float (&v)[16], int n) {
+// Lanes 8..15 of each row of 16 get `b` of the lane eight before them, the others keep `a`; and the other way round.
+__device__ __forceinline__ uint32_t upper_from(uint32_t a, uint32_t b) { return (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xF, 0xC, false); }
+__device__ __forceinline__ uint32_t lower_from(uint32_t a, uint32_t b) { return (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xF, 0x3, false); }
+
+// Stores of sixteen tokens' features.  v[j]: features 16 j + 4 q .. + 3 (q = lane / 16) of token lane % 16 of the panel and tile at o (rows
+// `stride` apart); `features` and `tokens` are inside the matrix.  The output is written once and large, so the stores are
+// streaming ones, and those only pay in whole 128-byte lines (16 layers of 4096 tokens by 8192 features by K = 128, all stores: 613 us in pieces of
+// 32 bytes, 237 through the L2).  So the lanes first exchange what they hold, in registers.
+// bf16: the lanes of q = 0, 1 (and 2, 3) swap halves, so that each has eight consecutive features of two tiles, w[0] of tile 0 (even q) or 2
+// and w[1] of tile 1 or 3; then tokens t and t + 8 swap, so that one store holds the lines of tokens 0..7 and the other of 8..15.
+__device__ __forceinline__ void store_tile(bf16_t* o, size_t stride, const f32x4 (&v)[4], int lane, int features, int tokens) {
+  const int q = lane >> 4, t = lane & 7, j = (lane >> 3) & 1;
+  uint32_t w[2][4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const u32x4 w = {pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]), pack_bf16x2(v[8 * h + 4], v[8 * h + 5]),
-                     pack_bf16x2(v[8 * h + 6], v[8 * h + 7])};
-    if (n >= 8 * (h + 1)) *reinterpret_cast<u32x4*>(o + 8 * h) = w;
-  }
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto x = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[i][2 * h], v[i][2 * h + 1]), pack_bf16x2(v[i + 2][2 * h], v[i + 2][2 * h + 1]), false, false);
+      w[i][h] = x[0];
+      w[i][2 + h] = x[1];
+    }
+  u32x4 a, b;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) { a[h] = upper_from(w[0][h], w[1][h]); b[h] = lower_from(w[1][h], w[0][h]); }
+  const int f = 16 * j + 32 * (q & 1) + 8 * (q >> 1);
+  bf16_t* p = o + t * stride + f;
+  if (f < features && t < tokens) __builtin_nontemporal_store(a, reinterpret_cast<u32x4*>(p));
+  if (f < features && t + 8 < tokens) __builtin_nontemporal_store(b, reinterpret_cast<u32x4*>(p + 8 * stride));
 }
-__device__ __forceinline__ void store_features(float* o, const float (&v)[16], int n) {
+// fp32: tokens t and t + 8 swap tiles 1 and 0, and 3 and 2
+__device__ __forceinline__ void store_tile(float* o, size_t stride, const f32x4 (&v)[4], int lane, int features, int tokens) {
+  const int q = lane >> 4, t = lane & 7, j = (lane >> 3) & 1;
 #pragma unroll
-  for (int h = 0; h < 4; ++h)
-    if (n >= 4 * (h + 1)) *reinterpret_cast<float4*>(o + 4 * h) = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
-}
-__device__ __forceinline__ void load_features(const float* p, float (&v)[16], int n, float none) {
+  for (int i = 0; i < 4; i += 2) {
+    u32x4 a, b;
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    float4 x = make_float4(none, none, none, none);
-    if (p && n >= 4 * (h + 1)) x = *reinterpret_cast<const float4*>(p + 4 * h);
-    v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
+    for (int h = 0; h < 4; ++h) {
+      const uint32_t x = __float_as_uint(v[i][h]), y = __float_as_uint(v[i + 1][h]);
+      a[h] = upper_from(x, y);
+      b[h] = lower_from(y, x);
+    }
+    const int f = 16 * (i + j) + 4 * q;
+    float* p = o + t * stride + f;
+    if (f < features && t < tokens) __builtin_nontemporal_store(a, reinterpret_cast<u32x4*>(p));
+    if (f < features && t + 8 < tokens) __builtin_nontemporal_store(b, reinterpret_cast<u32x4*>(p + 8 * stride));
   }
 }
 
+template <int i> using I = std::integral_constant<int, i>;
 struct ProductArgs { int M, N, KS; Mx4 a, b; const float* bias; const float* theta; void* out; };
 
-// Bias, threshold, rounding and the stores of MT tiles of 16 tokens by one panel of features
-template <typename T, int MT>
+// Accumulators of MT tiles of 16 tokens by one panel of features begin at the features' bias: an addition that costs nothing.
+template <int MT>
+__device__ __forceinline__ void begin(const ProductArgs& p, int l, int panel, int lane, f32x4 (&acc)[MT][4]) {
+  const int f = panel * 64 + 4 * (lane >> 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f32x4 b = {0.f, 0.f, 0.f, 0.f};
+    if (p.bias && f + 16 * j < p.N) b = *reinterpret_cast<const f32x4*>(p.bias + (size_t)l * p.N + f + 16 * j);      // N is a multiple of 8
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i][j] = b;
+  }
+}
+// Threshold, rounding and stores
+template <typename T, bool THETA, int MT>
 __device__ __forceinline__ void finish(const ProductArgs& p, int l, int token0, int panel, int lane, const f32x4 (&acc)[MT][4]) {
-  const int n0 = panel * 64 + (lane >> 4) * 16, n = p.N - n0;
-  if (n <= 0) return;
-  float bias[16], theta[16];
-  load_features(p.bias ? p.bias + (size_t)l * p.N + n0 : nullptr, bias, n, 0.f);
-  load_features(p.theta ? p.theta + (size_t)l * p.N + n0 : nullptr, theta, n, 0.f);
+  const int f = panel * 64 + 4 * (lane >> 4);
+  f32x4 theta[4];
+  if (THETA) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      theta[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (f + 16 * j < p.N) theta[j] = *reinterpret_cast<const f32x4*>(p.theta + (size_t)l * p.N + f + 16 * j);
+    }
+  }
+  T* o = static_cast<T*>(p.out) + ((size_t)l * p.M + token0) * p.N + panel * 64;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int m = token0 + i * 16 + (lane & 15);
-    if (m >= p.M) continue;
-    float v[16];
+    const int m = token0 + i * 16;
+    if (m >= p.M) break;
+    f32x4 v[4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      v[j] = acc[i][j >> 2][j & 3] + bias[j];
-      if (p.theta && !(v[j] > theta[j])) v[j] = 0.f;
-    }
-    store_features(static_cast<T*>(p.out) + ((size_t)l * p.M + m) * p.N + n0, v, n);
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[j][k] = !THETA || acc[i][j][k] > theta[j][k] ? acc[i][j][k] : 0.f;
+    store_tile(o + (size_t)(i * 16) * p.N, p.N, v, lane, p.N - panel * 64, p.M - m);
   }
 }
 
-// Many tokens: one workgroup takes 128 tokens by 256 features, each of its four wavefronts one panel of 64 features by all the
-// tokens (8 x 4 accumulators of 16 x 16).  A panel is read by one wavefront only and goes from memory into its registers; the tokens
-// are staged in LDS in two stages of one step each.  Two workgroups share a compute unit, so that one's prologue and epilogue
-// run under the other's matrix instructions.
-constexpr int PT = 8;      // tiles of 16 tokens
-template <typename T>
-__global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, int tiles_m, int tiles_n) {
-  __shared__ u32x4 stage[2][PT * 64];
+// Many tokens: a workgroup takes tiles of 128 tokens by 256 features one after the other, each of its four wavefronts one panel of 64
+// features by all the tokens (8 x 4 accumulators of 16 x 16).  A panel is read by one wavefront only and goes from memory into its
+// registers, one step ahead; the tokens are fetched three steps ahead and staged in LDS, in three stages of one step each.  Both run on
+// into the next tile.  Two workgroups share a compute unit, so that one's epilogue runs under the other's matrix instructions.
+constexpr int PT = 8;             // tiles of 16 tokens
+constexpr int AHEAD = 3;          // of these, the operands under way from LDS
+constexpr int WORKGROUPS = 512;   // two on each of 256 compute units
+
+// Quotients n / d for n < 2^31 by a multiplication: m = floor(2^(31+s) / d) + 1 with 2^(s-1) < d <= 2^s is too large by less than 2^s / 2^(31+s)
+// of itself.  (Division instructions do not exist; a wavefront would spend as long on three quotients as on two steps.)
+struct Quotient {
+  uint32_t m, s;
+  explicit Quotient(uint32_t d) : s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)((1ull << (31 + s)) / d) + 1;
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> (31 + s)); }
+};
+// The order of the tiles: layer by layer; eight tiles of tokens at a time (fewer in the last group) through all the features
+struct TileOrder {
+  uint32_t tiles, per_layer, per_group; int tiles_m; Quotient layer, group, last_rows;
+  TileOrder(int L, int tiles_m, int tiles_n) : tiles((uint32_t)((size_t)L * tiles_m * tiles_n)), per_layer((uint32_t)tiles_m * tiles_n), per_group(8 * tiles_n),
+    tiles_m(tiles_m), layer(per_layer), group(per_group), last_rows((tiles_m & 7) ? tiles_m & 7 : 8) {}
+};
+// Where a workgroup stands: a step of one of its tiles
+struct Cursor {
+  uint32_t t; int ks, l, tm, panel; bool ok;
+};
+template <typename T, bool THETA>
+__global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, TileOrder order) {
+  __shared__ u32x4 stage[3][PT * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KS = p.KS, panels_m = (p.M + 63) >> 6, panels_n = (p.N + 63) >> 6;
   // Workgroups are dealt to the eight XCDs in turn: each XCD takes a run of consecutive tiles, which go through the features for
   // eight tiles of tokens at a time, so that the tiles at work on an XCD share their operands in its L2.
-  const uint32_t n = gridDim.x, x = blockIdx.x & 7, t = x * (n >> 3) + min(x, n & 7) + (blockIdx.x >> 3), per_layer = (uint32_t)tiles_m * tiles_n;
-  const int l = t / per_layer, r = t - l * per_layer, group = r / (8 * tiles_n), rows = min(8, tiles_m - group * 8), in_group = r - group * 8 * tiles_n;
-  const int tm = group * 8 + in_group % rows, tn = in_group / rows;
-  const int panel = tn * 4 + wave;
+  const uint32_t xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3;      // the grid is a multiple of 8
+  const uint32_t first = xcd * (order.tiles >> 3) + min(xcd, order.tiles & 7), end = first + (order.tiles >> 3) + (xcd < (order.tiles & 7) ? 1 : 0);
+  auto locate = [&](Cursor& c) {
+    c.ok = c.t < end;
+    const uint32_t t = c.ok ? c.t : first;
+    c.l = order.layer.of(t);
+    const uint32_t r = t - c.l * order.per_layer, group = order.group.of(r), in_group = r - group * order.per_group;
+    const int rows = min(8, order.tiles_m - (int)group * 8), tn = rows == 8 ? in_group >> 3 : order.last_rows.of(in_group);
+    c.tm = group * 8 + in_group - tn * rows;
+    c.panel = tn * 4 + wave;
+  };
+  Cursor at{first + (blockIdx.x >> 3), 0, 0, 0, 0, false};
+  locate(at);
+  if (!at.ok) return;
   // (tiles and panels beyond the matrix: the last one again; what it gives is not stored)
-  const PanelPtr B(p.b, (size_t)l * panels_n + min(panel, panels_n - 1), KS, lane);
-  const uint8_t* ac[2];
-  const uint32_t* as[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    ac[i] = p.a.codes + (((size_t)l * panels_m * 4 + min(tm * PT + wave + 4 * i, panels_m * 4 - 1)) * KS << 10) + lane * 16;
-    as[i] = reinterpret_cast<const uint32_t*>(p.a.scales + (((size_t)l * panels_m + min(tm * 2 + i, panels_m - 1)) * KS << 8)) + lane;
-  }
+  auto panel_of = [&](const Cursor& c) { return Panel(p.b, (size_t)c.l * panels_n + min(c.panel, panels_n - 1), KS); };
+  struct Tokens { Source codes, scales; uint32_t a1, s1; };
+  auto tokens_of = [&](const Cursor& c) {
+    const uint32_t second = c.tm * 2 + 1 < panels_m ? 1 : 0;      // the second panel of tokens
+    return Tokens{Source(p.a.codes + (((size_t)c.l * panels_m * 4 + c.tm * PT) * KS << 10)),
+                  Source(p.a.scales + (((size_t)c.l * panels_m + c.tm * 2) * KS << 8)), (second * 4 * KS) << 10, (second * KS) << 8};
+  };
+  Cursor ca = at, cb = at;      // of the next fetch of tokens and of features (behind the last tile they fetch the first of this XCD, for nothing)
+  Panel B = panel_of(cb);
+  Tokens A = tokens_of(ca), S = A;      // S: for the tokens' scales, which go with the features
   f32x4 acc[PT][4];
-#pragma unroll
-  for (int i = 0; i < PT; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 next[2];
+  u32x4 next[2], fa[4];
   PanelFrag fb[2];
   uint32_t sa[2][2];
-  auto fetch_a = [&](int ks) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) next[i] = *reinterpret_cast<const u32x4*>(ac[i] + ((size_t)ks << 10));
+  auto load_a = [&]() {
+    next[0] = A.codes.lanes16(lane, (uint32_t)(wave * KS + ca.ks) << 10);
+    next[1] = A.codes.lanes16(lane, A.a1 + ((uint32_t)(wave * KS + ca.ks) << 10));
   };
-  auto fetch_b = [&](int ks, int buf) {
-    B.load(fb[buf], ks);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) sa[buf][i] = as[i][ks << 6];
-  };
-  auto put = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) stage[buf][(wave + 4 * i) * 64 + lane] = next[i];
-  };
-  fetch_a(0);
-  fetch_b(0, 0);
-  put(0);
-  if (KS > 1) fetch_a(1);
-  __syncthreads();
-  auto step = [&](int ks, int buf) {
-    if (ks + 1 < KS) {
-      put(buf ^ 1);
-      fetch_b(ks + 1, buf ^ 1);
-      if (ks + 2 < KS) fetch_a(ks + 2);
+  auto advance_a = [&]() {
+    if (__builtin_expect(++ca.ks == KS, 0)) {
+      ca.ks = 0;
+      ca.t += per_xcd;
+      locate(ca);
+      A = tokens_of(ca);
     }
+  };
+  auto load_b = [&](int buf, int j) { fb[buf].c[j] = B.tile(j, cb.ks, lane); };
+  auto load_scales = [&](int buf) {
+    fb[buf].s = B.scale(cb.ks, lane);
+    sa[buf][0] = S.scales.lanes4(lane, (uint32_t)cb.ks << 8);
+    sa[buf][1] = S.scales.lanes4(lane, S.s1 + ((uint32_t)cb.ks << 8));
+  };
+  auto advance_b = [&]() {
+    if (__builtin_expect(++cb.ks == KS, 0)) {
+      cb.ks = 0;
+      cb.t += per_xcd;
+      locate(cb);
+      B = panel_of(cb);
+      S = tokens_of(cb);
+    }
+  };
+  auto put = [&](int st) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) stage[st][(wave + 4 * i) * 64 + lane] = next[i];
+  };
+  load_a(); advance_a(); put(0);
+  load_a(); advance_a(); put(1);
+  load_a();
+  for (int j = 0; j < 4; ++j) load_b(0, j);
+  load_scales(0);
+  begin(p, at.l, at.panel, lane, acc);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fa[i] = stage[0][i * 64 + lane];
+  // One step: the features of the next step are fetched, the tokens of two steps on go to LDS (into the stage that the step before read)
+  // and those of three steps on are fetched, one or two instructions of this at a time between the matrix instructions, which leave twelve
+  // cycles each for others to issue.  Each tile's operand is read three tiles ahead, across the barrier as well: what is read before it
+  // belongs to the next step and was written before the last barrier.
+  int s0 = 0, s1 = 1, s2 = 2;
+  auto step = [&](auto i2) {
+    constexpr int b = decltype(i2)::value;
+    // (The branches of a step come before its matrix instructions: the compiler moved them into the block behind a branch, past the barrier.)
+    advance_a();
+    advance_b();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
-      const u32x4 a = stage[buf][i * 64 + lane];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = mfma(i, fb[buf].c[j], fb[buf].s[j], a, sa[buf][i >> 2], acc[i][j]);
+      const int r = i + AHEAD;
+      if (i == 0) load_scales(b ^ 1);
+      if (i < 4) load_b(b ^ 1, i);
+      if (i == PT - AHEAD - 1) put(s2);      // (at least AHEAD reads come behind it)
+      if (i == 5) load_a();
+      fa[r & 3] = stage[r < PT ? s0 : s1][(r & (PT - 1)) * 64 + lane];
+      mfma4(i, fb[b], fa[i & 3], sa[b][i >> 2], acc[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
+    // Not __syncthreads(), which waits for the reads under way as well: all but the last AHEAD of this wavefront's LDS accesses, its
+    // writes among them, are done here (they complete in order).
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F | AHEAD << 8);      // lgkmcnt(AHEAD)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const int s = s0;
+    s0 = s1; s1 = s2; s2 = s;
+    if (__builtin_expect(++at.ks < KS, 1)) return true;
+    finish<T, THETA>(p, at.l, at.tm * PT * 16, at.panel, lane, acc);
+    at.ks = 0;
+    at.t += per_xcd;
+    locate(at);
+    if (at.ok) begin(p, at.l, at.panel, lane, acc);
+    return at.ok;
   };
-  int ks = 0;
-  for (; ks + 2 <= KS; ks += 2) { step(ks, 0); step(ks + 1, 1); }
-  if (ks < KS) step(ks, 0);
-  finish<T, PT>(p, l, tm * PT * 16, panel, lane, acc);
+  while (step(I<0>()) && step(I<1>())) {}
 }
 
 // Few tokens: bound by the bytes of B.  One workgroup takes one panel of 64 features by MT tiles of 16 tokens; its four wavefronts take
 // every fourth step of the contraction, straight from memory, two steps in flight, and add up in LDS in a fixed order.
-template <typename T, int MT>
+template <typename T, bool THETA, int MT>
 __global__ __launch_bounds__(256) void mx4_product_few_kernel(ProductArgs p) {
   __shared__ f32x4 part[3][MT * 4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KS = p.KS, panels_m = (p.M + 63) >> 6, panels_n = (p.N + 63) >> 6, panel = blockIdx.x, token0 = blockIdx.y * MT * 16, l = blockIdx.z;
-  const PanelPtr B(p.b, (size_t)l * panels_n + panel, KS, lane);
-  const uint8_t* ac = p.a.codes + (((size_t)l * panels_m * 4 + (token0 >> 4)) * KS << 10) + lane * 16;
-  const uint32_t* as = reinterpret_cast<const uint32_t*>(p.a.scales + (((size_t)l * panels_m + (token0 >> 6)) * KS << 8)) + lane;
+  const Panel B(p.b, (size_t)l * panels_n + panel, KS);
+  const Source ac(p.a.codes + (((size_t)l * panels_m * 4 + (token0 >> 4)) * KS << 10)), as(p.a.scales + (((size_t)l * panels_m + (token0 >> 6)) * KS << 8));
   f32x4 acc[MT][4];
+  begin(p, l, panel, lane, acc);
+  if (wave > 0) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < MT * 4; ++i) acc[i >> 2][i & 3] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   PanelFrag fb[2];
   u32x4 fa[2][MT];
   uint32_t sa[2];
   auto fetch = [&](int ks, int buf) {
-    B.load(fb[buf], ks);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) fa[buf][i] = *reinterpret_cast<const u32x4*>(ac + (((size_t)i * KS + ks) << 10));
-    sa[buf] = as[ks << 6];
+    for (int j = 0; j < 4; ++j) fb[buf].c[j] = B.tile(j, ks, lane);
+    fb[buf].s = B.scale(ks, lane);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[buf][i] = ac.lanes16(lane, (uint32_t)(i * KS + ks) << 10);
+    sa[buf] = as.lanes4(lane, (uint32_t)ks << 8);
   };
   auto compute = [&](int buf) {
     const uint32_t s = MT == 4 ? sa[buf] : sa[buf] >> (8 * ((token0 >> 4) & 3));
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = mfma(i, fb[buf].c[j], fb[buf].s[j], fa[buf][i], s, acc[i][j]);
+    for (int i = 0; i < MT; ++i) mfma4(i, fb[buf], fa[buf][i], s, acc[i]);
   };
   if (wave < KS) fetch(wave, 0);
   for (int ks = wave; ks < KS; ks += 8) {
@@ -380,21 +506,23 @@ __global__ __launch_bounds__(256) void mx4_product_few_kernel(ProductArgs p) {
     const f32x4 x = part[0][i][lane], y = part[1][i][lane], z = part[2][i][lane];
     acc[i >> 2][i & 3] = (acc[i >> 2][i & 3] + x) + (y + z);
   }
-  finish<T, MT>(p, l, token0, panel, lane, acc);
+  finish<T, THETA>(p, l, token0, panel, lane, acc);
 }
 
-template <typename T>
+template <typename T, bool THETA>
 hipError_t launch_product(hipStream_t s, int L, const ProductArgs& p) {
   const int panels_n = (p.N + 63) / 64;
   if (p.M <= 64) {
     const dim3 wg(256);
-    if (p.M <= 16) hipLaunchKernelGGL((mx4_product_few_kernel<T, 1>), dim3(panels_n, 1, L), wg, 0, s, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((mx4_product_few_kernel<T, 2>), dim3(panels_n, 1, L), wg, 0, s, p);
-    else hipLaunchKernelGGL((mx4_product_few_kernel<T, 4>), dim3(panels_n, 1, L), wg, 0, s, p);
+    if (p.M <= 16) hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 1>), dim3(panels_n, 1, L), wg, 0, s, p);
+    else if (p.M <= 32) hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 2>), dim3(panels_n, 1, L), wg, 0, s, p);
+    else hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 4>), dim3(panels_n, 1, L), wg, 0, s, p);
     return hipGetLastError();
   }
   const int tiles_m = (p.M + PT * 16 - 1) / (PT * 16), tiles_n = (panels_n + 3) / 4;
-  hipLaunchKernelGGL(mx4_product_kernel<T>, dim3((uint32_t)((size_t)L * tiles_m * tiles_n)), dim3(256), 0, s, p, tiles_m, tiles_n);
+  const TileOrder order(L, tiles_m, tiles_n);
+  const uint32_t grid = order.tiles >= WORKGROUPS ? WORKGROUPS : (order.tiles + 7) / 8 * 8;
+  hipLaunchKernelGGL((mx4_product_kernel<T, THETA>), dim3(grid), dim3(256), 0, s, p, order);
   return hipGetLastError();
 }
 
@@ -423,7 +551,8 @@ hipError_t launch_mx4_dequantise(hipStream_t s, bool bf16, int L, int rows, int 
 hipError_t launch_mx4_product(hipStream_t s, bool bf16, int L, int M, int N, int K, Mx4 a, Mx4 b, const float* bias, const float* theta,
                               void* out) {
   const ProductArgs p{M, N, mx4_steps(K), a, b, bias, theta, out};
-  return bf16 ? launch_product<bf16_t>(s, L, p) : launch_product<float>(s, L, p);
+  if (bf16) return theta ? launch_product<bf16_t, true>(s, L, p) : launch_product<bf16_t, false>(s, L, p);
+  return theta ? launch_product<float, true>(s, L, p) : launch_product<float, false>(s, L, p);
 }
 
 }  // namespace clt
