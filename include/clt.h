@@ -267,7 +267,7 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
  * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
  * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN gets codes 0 and a NaN as its scale.
- * Except for h, an output must not overlap an input.  L, B >= 1, d a positive multiple of 8, eps > 0. */
+ * Except for h, an output must not overlap an input.  1 <= L <= 128, B >= 1, L B < 2^30, d a positive multiple of 8, eps > 0. */
 int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
                  const float* weight, float eps, void* h, void* y, int8_t* q, float* q_scale, float* rstd);
 

@@ -294,33 +294,53 @@ def clt_backward_adam_step(H: Handle, x, z, act_class, t: int, lr: float, params
 
 # ---- around the training step: no handle ------------------------------------------------------------------------
 
-def _storage(t, name):
-    """(dtype code, torch dtype) of a native activation or matrix tensor [L, B, d], which sets the type of the call."""
+def _device_of(t, name):
+    """Device index of a call's first tensor.  The kernels run on the current device's current stream: it has to be there."""
     if t is None:
         raise ValueError(f"{name} is required")
-    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16):
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _arg(t, dev, shape, dtype, name):
+    """_ptr for a required tensor of a call on device `dev`."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on cuda:{dev}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _may(t, dev, shape, dtype, name):
+    return None if t is None else _arg(t, dev, shape, dtype, name)
+
+
+_TYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _storage(t, name):
+    """Type code of a native activation or matrix tensor [L, B, d], which sets the type of the call."""
+    if t.dim() != 3 or t.dtype not in _TYPES:
         raise ValueError(f"{name}: expected a 3-dimensional float32 or bfloat16 tensor, got {tuple(t.shape)} {t.dtype}")
-    return (DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16), t.dtype
-
-
-def _here(*tensors):
-    """The kernels run on the current device's current stream: every tensor has to live there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    return _TYPES[t.dtype]
 
 
 def clt_rms_norm(x, weight, eps, y=None, q=None, q_scale=None, residual=None, h=None, rstd=None):
     """RMS norm of residual streams x (+ residual, the sum stored in h) into y and / or int8 codes q with row scales
     q_scale (include/clt.h).  x [L, B, d] float32 or bfloat16, weight [L, d] float32; rstd [L, B] for the backward pass."""
-    dt, T = _storage(x, "x")
-    f32, s = torch.float32, tuple(x.shape)
-    args = (dt, _ptr(x, s, T, "x"), _ptr(residual, s, T, "residual", True), _ptr(weight, (s[0], s[2]), f32, "weight"), float(eps),
-            _ptr(h, s, T, "h", True), _ptr(y, s, T, "y", True), _ptr(q, s, torch.int8, "q", True),
-            _ptr(q_scale, s[:2], f32, "q_scale", True), _ptr(rstd, s[:2], f32, "rstd", True))
-    _here(x, weight, y, q, q_scale, residual, h, rstd)
-    _check(_lib.clt_rms_norm(_stream(), *s, *args))
+    dev = _device_of(x, "x")
+    dt, T, s, f32 = _storage(x, "x"), x.dtype, x.shape, torch.float32
+    L, B, d = s
+    _check(_lib.clt_rms_norm(
+        _stream(), L, B, d, dt, _arg(x, dev, s, T, "x"), _may(residual, dev, s, T, "residual"), _arg(weight, dev, (L, d), f32, "weight"), eps,
+        _may(h, dev, s, T, "h"), _may(y, dev, s, T, "y"), _may(q, dev, s, torch.int8, "q"), _may(q_scale, dev, (L, B), f32, "q_scale"),
+        _may(rstd, dev, (L, B), f32, "rstd")))
 
 
 def clt_rms_norm_backward_workspace_bytes(L, B, d) -> int:
@@ -329,17 +349,24 @@ def clt_rms_norm_backward_workspace_bytes(L, B, d) -> int:
     return n.value
 
 
+def _room(t, dev):
+    """(pointer, bytes) of an optional workspace."""
+    if t is None:
+        return None, 0
+    if t.dtype != torch.uint8 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
+    return t.data_ptr(), t.numel()
+
+
 def clt_rms_norm_backward(h, weight, rstd, dy, dx, dweight=None, workspace=None, dh=None):
     """Gradients of clt_rms_norm; dx may be dy or dh.  workspace: uint8, clt_rms_norm_backward_workspace_bytes, with dweight."""
-    dt, T = _storage(h, "h")
-    f32, s = torch.float32, tuple(h.shape)
-    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous uint8 device tensor")
-    args = (dt, _ptr(h, s, T, "h"), _ptr(weight, (s[0], s[2]), f32, "weight"), _ptr(rstd, s[:2], f32, "rstd"), _ptr(dy, s, T, "dy"),
-            _ptr(dh, s, T, "dh", True), _ptr(dx, s, T, "dx"), _ptr(dweight, (s[0], s[2]), f32, "dweight", True),
-            workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0)
-    _here(h, weight, rstd, dy, dx, dweight, workspace, dh)
-    _check(_lib.clt_rms_norm_backward(_stream(), *s, *args))
+    dev = _device_of(h, "h")
+    dt, T, s, f32 = _storage(h, "h"), h.dtype, h.shape, torch.float32
+    L, B, d = s
+    _check(_lib.clt_rms_norm_backward(
+        _stream(), L, B, d, dt, _arg(h, dev, s, T, "h"), _arg(weight, dev, (L, d), f32, "weight"), _arg(rstd, dev, (L, B), f32, "rstd"),
+        _arg(dy, dev, s, T, "dy"), _may(dh, dev, s, T, "dh"), _arg(dx, dev, s, T, "dx"), _may(dweight, dev, (L, d), f32, "dweight"),
+        *_room(workspace, dev)))
 
 
 ADAMW_BLOCK = 128
@@ -351,27 +378,25 @@ class AdamWTensor:
     contiguous; p, g, m, v and master have the same number of elements."""
 
     def __init__(self, p, g, m, v, m_scale=None, v_scale=None, master=None, weight_decay=0.0):
+        dev = _device_of(p, "p")
         n = p.numel()
-        eight = m.dtype == torch.uint8
-        types = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
-        if p.dtype not in types or g.dtype not in types:
-            raise ValueError(f"p and g must be float32 or bfloat16, got {p.dtype} and {g.dtype}")
+        eight = m is not None and m.dtype == torch.uint8
+        if p.dtype not in _TYPES or g is None or g.dtype not in _TYPES:
+            raise ValueError("p and g must be float32 or bfloat16 tensors")
         if eight != (m_scale is not None) or eight != (v_scale is not None):
             raise ValueError("m_scale and v_scale belong to 8-bit (uint8) moments")
         state = torch.uint8 if eight else torch.float32
-        flat = ((p, p.dtype, "p"), (g, g.dtype, "g"), (m, state, "m"), (v, state, "v"), (master, torch.float32, "master"))
-        for t, dt, name in flat:
-            _ptr(t, tuple(t.shape) if t is not None and t.numel() == n else (n,), dt, name, name == "master")
+        for t, dt, name in ((p, p.dtype, "p"), (g, g.dtype, "g"), (m, state, "m"), (v, state, "v")):
+            _arg(t, dev, t.shape if t is not None and t.numel() == n else (n,), dt, name)
+        if master is not None:
+            _arg(master, dev, master.shape if master.numel() == n else (n,), torch.float32, "master")
         blocks = ((n + ADAMW_BLOCK - 1) // ADAMW_BLOCK,)
-        _ptr(m_scale, blocks, torch.uint8, "m_scale", True)
-        _ptr(v_scale, blocks, torch.uint8, "v_scale", True)
+        _may(m_scale, dev, blocks, torch.uint8, "m_scale")
+        _may(v_scale, dev, blocks, torch.uint8, "v_scale")
+        self.device = dev
         self.tensors = (p, g, m, v, m_scale, v_scale, master)      # kept alive
-        self.c = clt_adamw_tensor(*(None if t is None else t.data_ptr() for t in self.tensors), n, types[p.dtype], types[g.dtype],
+        self.c = clt_adamw_tensor(*(None if t is None else t.data_ptr() for t in self.tensors), n, _TYPES[p.dtype], _TYPES[g.dtype],
                                   8 if eight else 32, float(weight_decay))
-
-
-def _adamw_array(tensors):
-    return (clt_adamw_tensor * max(1, len(tensors)))(*(t.c for t in tensors))
 
 
 def clt_adamw_step(tensors, t, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
@@ -384,9 +409,10 @@ class AdamW:
 
     def __init__(self, tensors, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
         self.tensors = list(tensors)
-        _here(*(x for t in self.tensors for x in t.tensors if x is not None))
-        self.device = torch.cuda.current_device() if self.tensors else None
-        self._array = _adamw_array(self.tensors)
+        self.device = self.tensors[0].device if self.tensors else None
+        if any(t.device != self.device for t in self.tensors):
+            raise ValueError("the tensors are on different devices")
+        self._array = (clt_adamw_tensor * max(1, len(self.tensors)))(*(t.c for t in self.tensors))
         self.scalars = (float(beta1), float(beta2), float(eps), int(seed))
 
     @staticmethod
@@ -403,7 +429,7 @@ class AdamW:
     def step(self, t, lr):
         if self.device is not None and torch.cuda.current_device() != self.device:
             raise ValueError(f"the tensors are on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
-        _check(_lib.clt_adamw_step(_stream(), len(self.tensors), self._array, int(t), float(lr), *self.scalars))
+        _check(_lib.clt_adamw_step(_stream(), len(self.tensors), self._array, t, lr, *self.scalars))
 
 
 def clt_mx4_bytes(L, rows, K):
@@ -413,53 +439,53 @@ def clt_mx4_bytes(L, rows, K):
     return c.value, s.value
 
 
+def _mx4_shapes(L, rows, K):
+    rp, ks = (rows + 63) // 64, (K + 127) // 128
+    return (L, 4 * rp, ks, 1024), (L, rp, ks, 256)
+
+
 def mx4_empty(L, rows, K, device="cuda:0"):
     """Room for a packed 4-bit matrix [L][rows][K]: (codes, scales), uint8."""
     clt_mx4_bytes(L, rows, K)
-    rp, ks = (rows + 63) // 64, (K + 127) // 128
-    return (torch.empty((L, 4 * rp, ks, 1024), dtype=torch.uint8, device=device),
-            torch.empty((L, rp, ks, 256), dtype=torch.uint8, device=device))
+    codes, scales = _mx4_shapes(L, rows, K)
+    return torch.empty(codes, dtype=torch.uint8, device=device), torch.empty(scales, dtype=torch.uint8, device=device)
 
 
-def _packed(codes, scales, L, rows, K, name):
-    rp, ks = (rows + 63) // 64, (K + 127) // 128
-    return (_ptr(codes, (L, 4 * rp, ks, 1024), torch.uint8, f"{name}codes"), _ptr(scales, (L, rp, ks, 256), torch.uint8, f"{name}scales"))
+def _packed(codes, scales, dev, L, rows, K, name):
+    c, s = _mx4_shapes(L, rows, K)
+    return _arg(codes, dev, c, torch.uint8, name + "codes"), _arg(scales, dev, s, torch.uint8, name + "scales")
 
 
 def clt_mx4_quantise(a, codes, scales, a_scale=None, transposed=False):
     """Packs a [L, rows, K] (float32, bfloat16, or int8 with a_scale [L, rows]; transposed: [L, K, rows]) into 4 bits."""
-    if a is not None and a.dtype == torch.int8:
+    dev = _device_of(a, "a")
+    if a.dtype == torch.int8:
         if a.dim() != 3:
             raise ValueError(f"a: expected a 3-dimensional tensor, got {tuple(a.shape)}")
-        dt, T, fmt = DTYPE_BF16, torch.int8, INPUT_INT8_ROWSCALE
+        dt, fmt = DTYPE_BF16, INPUT_INT8_ROWSCALE
     else:
-        (dt, T), fmt = _storage(a, "a"), INPUT_NATIVE
-    s = tuple(a.shape)
+        dt, fmt = _storage(a, "a"), INPUT_NATIVE
+    s = a.shape
     L, rows, K = (s[0], s[2], s[1]) if transposed else s
-    args = (L, rows, K, dt, fmt, int(transposed), _ptr(a, s, T, "a"), _ptr(a_scale, (L, rows), torch.float32, "a_scale", True),
-            *_packed(codes, scales, L, rows, K, ""))
-    _here(a, a_scale, codes, scales)
-    _check(_lib.clt_mx4_quantise(_stream(), *args))
+    _check(_lib.clt_mx4_quantise(_stream(), L, rows, K, dt, fmt, int(transposed), _arg(a, dev, s, a.dtype, "a"),
+                                 _may(a_scale, dev, (L, rows), torch.float32, "a_scale"), *_packed(codes, scales, dev, L, rows, K, "")))
 
 
 def clt_mx4_dequantise(codes, scales, out):
     """The values of a packed matrix into out [L, rows, K] float32 or bfloat16."""
-    dt, T = _storage(out, "out")
-    L, rows, K = out.shape
-    args = (L, rows, K, dt, *_packed(codes, scales, L, rows, K, ""), _ptr(out, (L, rows, K), T, "out"))
-    _here(codes, scales, out)
-    _check(_lib.clt_mx4_dequantise(_stream(), *args))
+    dev = _device_of(out, "out")
+    dt, s = _storage(out, "out"), out.shape
+    L, rows, K = s
+    _check(_lib.clt_mx4_dequantise(_stream(), L, rows, K, dt, *_packed(codes, scales, dev, L, rows, K, ""), _arg(out, dev, s, out.dtype, "out")))
 
 
 def clt_mx4_product(a_codes, a_scales, b_codes, b_scales, out, K, bias=None, theta=None):
     """out [L, M, N] = A B^T + bias of packed A [L][M][K] and B [L][N][K], with theta kept where above it, else 0."""
-    dt, T = _storage(out, "out")
-    L, M, N = out.shape
-    f32 = torch.float32
-    args = (L, M, N, int(K), *_packed(a_codes, a_scales, L, M, K, "a_"), *_packed(b_codes, b_scales, L, N, K, "b_"),
-            _ptr(bias, (L, N), f32, "bias", True), _ptr(theta, (L, N), f32, "theta", True), dt, _ptr(out, (L, M, N), T, "out"))
-    _here(a_codes, a_scales, b_codes, b_scales, out, bias, theta)
-    _check(_lib.clt_mx4_product(_stream(), *args))
+    dev = _device_of(out, "out")
+    dt, s, f32 = _storage(out, "out"), out.shape, torch.float32
+    L, M, N = s
+    _check(_lib.clt_mx4_product(_stream(), L, M, N, K, *_packed(a_codes, a_scales, dev, L, M, K, "a_"), *_packed(b_codes, b_scales, dev, L, N, K, "b_"),
+                                _may(bias, dev, (L, N), f32, "bias"), _may(theta, dev, (L, N), f32, "theta"), dt, _arg(out, dev, s, out.dtype, "out")))
 
 
 _VIEWS = {"norms": (0, torch.float32, lambda c: (c.L, c.F)), "d_yhat": (1, None, lambda c: (c.L, c.B, c.d)),

@@ -824,8 +824,8 @@ int clt_adam_step(clt_handle* h, void* stream, int64_t t, float lr, const clt_te
   } while (0)
 
 static int check_rows(const char* who, int32_t L, int32_t B, int32_t d) {
-  if (L < 1 || L > 128 || B < 1 || d < 8 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 31)
-    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^31, d a positive multiple of 8)", who, L, B, d);
+  if (L < 1 || L > 128 || B < 1 || d < 8 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 30)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^30, d a positive multiple of 8)", who, L, B, d);
   return CLT_OK;
 }
 

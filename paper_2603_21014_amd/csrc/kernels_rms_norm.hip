@@ -19,9 +19,130 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 // Rows whose largest |h w| is below this count as all-zero (127 / max must not overflow).
 constexpr float ROW_IS_ZERO = 0x1p-100f;
 
-// One workgroup per row, the row read twice.
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+template <typename T> struct Vec16 { static constexpr int N = 16 / sizeof(T); };      // elements in 16 bytes
+__device__ __forceinline__ void widen16(u32x4 r, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(r[i] << 16); f[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void widen16(u32x4 r, float (&f)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ u32x4 narrow16(const float (&f)[8]) {
+  return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+}
+__device__ __forceinline__ u32x4 narrow16(const float (&f)[4]) {
+  return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+}
+
+// What the codes and the scale of a row follow from
+struct RowScale { float rstd, k, scale; bool broken; };
+__device__ __forceinline__ RowScale row_scale(float sum, uint32_t top, float eps, int d) {
+  RowScale r;
+  r.rstd = 1.0f / sqrtf(sum / (float)d + eps);
+  const float amax = __uint_as_float(top);
+  const bool zero = amax < ROW_IS_ZERO;
+  r.broken = top >= 0x7f800000u;
+  r.k = r.broken || zero ? 0.f : 127.0f / amax;
+  r.scale = r.broken ? __uint_as_float(0x7fc00000u) : zero ? 1.f : amax * r.rstd / 127.0f;
+  return r;
+}
+__device__ __forceinline__ uint32_t code(float t, const RowScale& r) { return (uint32_t)(int)(r.broken ? 0.f : rintf(t * r.k)) & 255u; }
+
+// A row is held in registers by one wavefront (W = 1, four rows at a time in a workgroup) or by a workgroup (W = 4), NV pieces of 16
+// bytes per lane, so that it is read once: the sum of squares and the largest |h weight| come from the same pass, and the codes
+// 127 y / max|y| need no second one because rstd cancels in them.  The weights stay in registers over the rows of a wavefront (they are
+// four bytes where a bf16 element is two).
+template <typename T, int NV, int W>
+__global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_each, RmsNormArgs a) {
+  constexpr int N = Vec16<T>::N;
+  __shared__ float sums[2][4];
+  __shared__ uint32_t tops[2][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = blockIdx.y;
+  const int b0 = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x) * rows_each, b1 = min(B, b0 + rows_each);
+  int e[NV];      // first element of each piece
+#pragma unroll
+  for (int v = 0; v < NV; ++v) e[v] = ((W == 1 ? 0 : wave * NV * 64) + v * 64 + lane) * N;
+  float w[NV][N];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (e[v] < d) x = *reinterpret_cast<const float4*>(a.weight + (size_t)l * d + e[v] + i);
+      w[v][i] = x.x; w[v][i + 1] = x.y; w[v][i + 2] = x.z; w[v][i + 3] = x.w;
+    }
+  for (int b = b0; b < b1; ++b) {
+    const size_t row = (size_t)l * B + b, o = row * d;
+    const T *x = static_cast<const T*>(a.x) + o, *res = static_cast<const T*>(a.residual) + o;
+    u32x4 raw[NV], add[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      raw[v] = add[v] = u32x4{0u, 0u, 0u, 0u};
+      if (e[v] < d) {
+        raw[v] = *reinterpret_cast<const u32x4*>(x + e[v]);
+        if (a.residual) add[v] = *reinterpret_cast<const u32x4*>(res + e[v]);
+      }
+    }
+    float t[NV][N], s = 0.f;
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float h[N], r[N];
+      widen16(raw[v], h);
+      if (a.residual) {
+        widen16(add[v], r);
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] += r[i];
+        raw[v] = narrow16(h);      // the norm is that of the stored sum, as a model that reads it again would have it
+        widen16(raw[v], h);
+        if (e[v] < d) *reinterpret_cast<u32x4*>(static_cast<T*>(a.h) + o + e[v]) = raw[v];
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s = fmaf(h[i], h[i], s);
+        t[v][i] = h[i] * w[v][i];
+        top = max(top, __float_as_uint(t[v][i]) & 0x7fffffffu);
+      }
+    }
+    s = wave_sum(s);
+    top = wave_max(top);
+    if (W == 4) {
+      const int buf = b & 1;      // (two buffers: one barrier per row)
+      if (lane == 0) { sums[buf][wave] = s; tops[buf][wave] = top; }
+      __syncthreads();
+      s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+      top = max(max(tops[buf][0], tops[buf][1]), max(tops[buf][2], tops[buf][3]));
+    }
+    const RowScale r = row_scale(s, top, a.eps, d);
+    if ((W == 1 ? lane : threadIdx.x) == 0) {
+      if (a.rstd) a.rstd[row] = r.rstd;
+      if (a.q) a.q_scale[row] = r.scale;
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (e[v] >= d) continue;
+      if (a.y) {
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = t[v][i] * r.rstd;
+        *reinterpret_cast<u32x4*>(static_cast<T*>(a.y) + o + e[v]) = narrow16(y);
+      }
+      if (a.q) {
+        uint32_t c[N / 4];
+#pragma unroll
+        for (int i = 0; i < N; i += 4) c[i / 4] = code(t[v][i], r) | code(t[v][i + 1], r) << 8 | code(t[v][i + 2], r) << 16 | code(t[v][i + 3], r) << 24;
+        if (N == 8) *reinterpret_cast<uint2*>(a.q + o + e[v]) = make_uint2(c[0], c[N / 4 - 1]);
+        else *reinterpret_cast<uint32_t*>(a.q + o + e[v]) = c[0];
+      }
+    }
+  }
+}
+
+// Rows too wide for that: one workgroup per row, the row read twice.
 template <typename T>
-__global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, RmsNormArgs a) {
+__global__ __launch_bounds__(256) void rms_norm_wide_kernel(int B, int d, RmsNormArgs a) {
   __shared__ float sums[4];
   __shared__ uint32_t tops[4];
   const size_t row = blockIdx.x, o = row * d;
@@ -50,29 +171,116 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, RmsNormArgs
   __syncthreads();
   s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
   top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-  const float rstd = 1.0f / sqrtf(s / (float)d + a.eps);
-  const float amax = __uint_as_float(top);
-  const bool broken = top >= 0x7f800000u, zero = amax < ROW_IS_ZERO;
-  const float k = broken || zero ? 0.f : 127.0f / amax;
+  const RowScale r = row_scale(s, top, a.eps, d);
   if (threadIdx.x == 0) {
-    if (a.rstd) a.rstd[row] = rstd;
-    if (a.q) a.q_scale[row] = broken ? __uint_as_float(0x7fc00000u) : zero ? 1.f : amax * rstd / 127.0f;
+    if (a.rstd) a.rstd[row] = r.rstd;
+    if (a.q) a.q_scale[row] = r.scale;
   }
   const T* h = a.residual ? hs + o : x;
   for (int i = threadIdx.x * 4; i < d; i += 1024) {
     const float4 h4 = Elem<T>::load4(h + i), w4 = *reinterpret_cast<const float4*>(w + i);
     const float t[4] = {h4.x * w4.x, h4.y * w4.y, h4.z * w4.z, h4.w * w4.w};
-    if (a.y) Elem<T>::store4(static_cast<T*>(a.y) + o + i, make_float4(t[0] * rstd, t[1] * rstd, t[2] * rstd, t[3] * rstd));
-    if (a.q) {
-      uint32_t c = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c |= ((uint32_t)(int)(broken ? 0.f : rintf(t[j] * k)) & 255u) << (8 * j);
-      *reinterpret_cast<uint32_t*>(a.q + o + i) = c;
-    }
+    if (a.y) Elem<T>::store4(static_cast<T*>(a.y) + o + i, make_float4(t[0] * r.rstd, t[1] * r.rstd, t[2] * r.rstd, t[3] * r.rstd));
+    if (a.q) *reinterpret_cast<uint32_t*>(a.q + o + i) = code(t[0], r) | code(t[1], r) << 8 | code(t[2], r) << 16 | code(t[3], r) << 24;
   }
 }
 
-// dx: one workgroup per row, the row read twice
+// ---- backward pass ---------------------------------------------------------------------------------------------------
+//
+// The same arrangement: h, dy (and dh) of a row are read once, for dx and for the row's share of dweight, which the lanes add up in
+// registers over all rows of their wavefront.  A workgroup leaves one partial sum of dweight, a second kernel adds those in order.
+template <typename T, int NV, int W>
+__global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, int rows_each, RmsNormBackwardArgs a) {
+  constexpr int N = Vec16<T>::N;
+  __shared__ float sums[2][4];
+  __shared__ float part[W == 1 ? 3 : 1][NV * 64 * N];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = blockIdx.y;
+  const int b0 = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x) * rows_each, b1 = min(B, b0 + rows_each);
+  int e[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) e[v] = ((W == 1 ? 0 : wave * NV * 64) + v * 64 + lane) * N;
+  float w[NV][N], dw[NV][N];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (e[v] < d) x = *reinterpret_cast<const float4*>(a.weight + (size_t)l * d + e[v] + i);
+      w[v][i] = x.x; w[v][i + 1] = x.y; w[v][i + 2] = x.z; w[v][i + 3] = x.w;
+      dw[v][i] = dw[v][i + 1] = dw[v][i + 2] = dw[v][i + 3] = 0.f;
+    }
+  for (int b = b0; b < b1; ++b) {
+    const size_t row = (size_t)l * B + b, o = row * d;
+    u32x4 rh[NV], rg[NV], re[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      rh[v] = rg[v] = re[v] = u32x4{0u, 0u, 0u, 0u};
+      if (e[v] < d) {
+        rh[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.h) + o + e[v]);
+        rg[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.dy) + o + e[v]);
+        if (a.dh) re[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.dh) + o + e[v]);
+      }
+    }
+    const float r = a.rstd[row];
+    float s = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float h[N], g[N];
+      widen16(rh[v], h);
+      widen16(rg[v], g);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float gh = g[i] * h[i];
+        s = fmaf(w[v][i], gh, s);
+        dw[v][i] = fmaf(gh, r, dw[v][i]);
+      }
+    }
+    s = wave_sum(s);
+    if (W == 4) {
+      const int buf = b & 1;
+      if (lane == 0) sums[buf][wave] = s;
+      __syncthreads();
+      s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+    }
+    const float c = s / (float)d * r * r * r;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float h[N], g[N], x[N];
+      widen16(rh[v], h);
+      widen16(rg[v], g);
+      widen16(re[v], x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = fmaf(r, w[v][i] * g[i], fmaf(-c, h[i], x[i]));
+      if (e[v] < d) *reinterpret_cast<u32x4*>(static_cast<T*>(a.dx) + o + e[v]) = narrow16(x);
+    }
+  }
+  if (!a.dweight) return;
+  if (W == 1) {      // the four wavefronts' sums, in order
+    if (wave > 0) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[wave - 1][(v * N + i) * 64 + lane] = dw[v][i];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int k = (v * N + i) * 64 + lane;
+        dw[v][i] = (dw[v][i] + part[0][k]) + (part[1][k] + part[2][k]);
+      }
+  }
+  float* out = a.part + ((size_t)l * gridDim.x + blockIdx.x) * d;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      if (e[v] < d) *reinterpret_cast<float4*>(out + e[v] + i) = make_float4(dw[v][i], dw[v][i + 1], dw[v][i + 2], dw[v][i + 3]);
+}
+
+// Rows too wide for that.  dx: one workgroup per row, the row read twice; dweight: sums over DW_ROWS rows, a lane per column
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_dx_kernel(int B, int d, RmsNormBackwardArgs a) {
   __shared__ float sums[4];
@@ -102,7 +310,7 @@ __global__ __launch_bounds__(256) void rms_norm_dx_kernel(int B, int d, RmsNormB
 constexpr int DW_ROWS = 32;      // rows of a partial sum
 inline int dw_blocks(int B) { return (B + DW_ROWS - 1) / DW_ROWS; }
 
-// dweight, first pass: sums over DW_ROWS rows; grid = (columns / 256, row blocks, layers)
+// grid = (columns / 256, row blocks, layers)
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_dw_kernel(int B, int d, RmsNormBackwardArgs a) {
   const int c = blockIdx.x * 256 + threadIdx.x, l = blockIdx.z;
@@ -115,34 +323,106 @@ __global__ __launch_bounds__(256) void rms_norm_dw_kernel(int B, int d, RmsNormB
   }
   a.part[((size_t)l * gridDim.y + blockIdx.y) * d + c] = s;
 }
-__global__ __launch_bounds__(256) void rms_norm_dw_finish_kernel(int blocks, int d, const float* __restrict__ part, float* __restrict__ dweight) {
-  const int c = blockIdx.x * 256 + threadIdx.x, l = blockIdx.y;
-  if (c >= d) return;
-  float s = 0.f;
-  for (int b = 0; b < blocks; ++b) s += part[((size_t)l * blocks + b) * d + c];
-  dweight[(size_t)l * d + c] = s;
+// The partial sums of 64 columns: sixteen wavefronts take every sixteenth each, eight loads in flight, and their sums are added in
+// order.  (One lane for all 300 partial sums of a column: 10 us, most of the whole backward pass of 300 rows.)
+constexpr int FINISH = 16;
+__global__ __launch_bounds__(64 * FINISH) void rms_norm_dw_finish_kernel(int blocks, int d, const float* __restrict__ part, float* __restrict__ dweight) {
+  __shared__ float sum[FINISH][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, l = blockIdx.y;
+  float s[8] = {};
+  if (c < d) {
+    const float* p = part + (size_t)l * blocks * d + c;
+    int b = wave;
+    for (; b + 7 * FINISH < blocks; b += 8 * FINISH) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += p[(size_t)(b + i * FINISH) * d];
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (b + i * FINISH < blocks) s[i] += p[(size_t)(b + i * FINISH) * d];
+  }
+  sum[wave][lane] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+  __syncthreads();
+  if (wave > 0 || c >= d) return;
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < FINISH; ++i) t += sum[i][lane];
+  dweight[(size_t)l * d + c] = t;
+}
+
+// How rows are cut: NV pieces of 16 bytes per lane of one wavefront (W = 1) or of four.  A wavefront takes up to 2048 elements of bf16 or
+// 1024 of fp32 (32 values and 32 weights in registers), a workgroup four times that; pieces 0: neither, the wide kernels.
+struct RowCut { int pieces, waves; };
+inline RowCut row_cut(bool bf16, int d) {
+  const int per = bf16 ? 512 : 256;      // elements of one piece of all lanes
+  for (int w = 1; w <= 4; w *= 4)
+    for (int nv = 1; nv <= 4; nv *= 2)
+      if (d <= per * nv * w) return {nv, w};
+  return {0, 0};
+}
+// Rows of a wavefront (or of a workgroup of four): enough wavefronts to fill the chip first, then rows that share the weights.
+inline int rows_each(int L, int B, int waves, int most) {
+  const int64_t n = ((int64_t)L * B * waves + 8191) / 8192;      // 8192 wavefronts: eight for every SIMD
+  return (int)(n < 1 ? 1 : n > most ? most : n);
 }
 
 }  // namespace
 
+#define ROW_KERNELS(KERNEL, T)                                                                                                      \
+  do {                                                                                                                              \
+    if (cut.waves == 1) {                                                                                                           \
+      if (cut.pieces == 1) hipLaunchKernelGGL((KERNEL<T, 1, 1>), grid, dim3(256), 0, s, B, d, each, a);                             \
+      else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 1>), grid, dim3(256), 0, s, B, d, each, a);                        \
+      else hipLaunchKernelGGL((KERNEL<T, 4, 1>), grid, dim3(256), 0, s, B, d, each, a);                                             \
+    } else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 4>), grid, dim3(256), 0, s, B, d, each, a);                        \
+    else hipLaunchKernelGGL((KERNEL<T, 4, 4>), grid, dim3(256), 0, s, B, d, each, a);                                               \
+  } while (0)
+
 hipError_t launch_rms_norm(hipStream_t s, bool bf16, int L, int B, int d, const RmsNormArgs& a) {
-  const dim3 grid((uint32_t)((size_t)L * B));
-  if (bf16) hipLaunchKernelGGL(rms_norm_kernel<bf16_t>, grid, dim3(256), 0, s, B, d, a);
-  else hipLaunchKernelGGL(rms_norm_kernel<float>, grid, dim3(256), 0, s, B, d, a);
+  const RowCut cut = row_cut(bf16, d);
+  if (!cut.pieces) {
+    const dim3 grid((uint32_t)((size_t)L * B));
+    if (bf16) hipLaunchKernelGGL(rms_norm_wide_kernel<bf16_t>, grid, dim3(256), 0, s, B, d, a);
+    else hipLaunchKernelGGL(rms_norm_wide_kernel<float>, grid, dim3(256), 0, s, B, d, a);
+    return hipGetLastError();
+  }
+  const int each = rows_each(L, B, cut.waves, 8), per = each * (cut.waves == 1 ? 4 : 1);
+  const dim3 grid((B + per - 1) / per, L);
+  if (bf16) ROW_KERNELS(rms_norm_kernel, bf16_t);
+  else ROW_KERNELS(rms_norm_kernel, float);
   return hipGetLastError();
 }
 
-size_t rms_norm_backward_floats(int L, int B, int d) { return (size_t)L * dw_blocks(B) * d; }
+// (the larger of both types' needs: the room is asked for without the type)
+static int dw_parts(bool bf16, int L, int B, int d) {
+  const RowCut cut = row_cut(bf16, d);
+  if (!cut.pieces) return dw_blocks(B);
+  const int per = rows_each(L, B, cut.waves, B) * (cut.waves == 1 ? 4 : 1);
+  return (B + per - 1) / per;
+}
+size_t rms_norm_backward_floats(int L, int B, int d) {
+  const int n = dw_parts(true, L, B, d), m = dw_parts(false, L, B, d);
+  return (size_t)L * (n > m ? n : m) * d;
+}
 
 hipError_t launch_rms_norm_backward(hipStream_t s, bool bf16, int L, int B, int d, const RmsNormBackwardArgs& a) {
-  const dim3 rows((uint32_t)((size_t)L * B)), cols((d + 255) / 256, dw_blocks(B), L);
-  if (a.dweight) {      // before dx, which may overwrite dy
-    if (bf16) hipLaunchKernelGGL(rms_norm_dw_kernel<bf16_t>, cols, dim3(256), 0, s, B, d, a);
-    else hipLaunchKernelGGL(rms_norm_dw_kernel<float>, cols, dim3(256), 0, s, B, d, a);
-    hipLaunchKernelGGL(rms_norm_dw_finish_kernel, dim3((d + 255) / 256, L), dim3(256), 0, s, dw_blocks(B), d, a.part, a.dweight);
+  const RowCut cut = row_cut(bf16, d);
+  const int parts = dw_parts(bf16, L, B, d);
+  if (cut.pieces) {
+    const int each = rows_each(L, B, cut.waves, B);
+    const dim3 grid(parts, L);
+    if (bf16) ROW_KERNELS(rms_norm_backward_kernel, bf16_t);
+    else ROW_KERNELS(rms_norm_backward_kernel, float);
+  } else {
+    const dim3 rows((uint32_t)((size_t)L * B)), cols((d + 255) / 256, parts, L);
+    if (a.dweight) {      // before dx, which may overwrite dy
+      if (bf16) hipLaunchKernelGGL(rms_norm_dw_kernel<bf16_t>, cols, dim3(256), 0, s, B, d, a);
+      else hipLaunchKernelGGL(rms_norm_dw_kernel<float>, cols, dim3(256), 0, s, B, d, a);
+    }
+    if (bf16) hipLaunchKernelGGL(rms_norm_dx_kernel<bf16_t>, rows, dim3(256), 0, s, B, d, a);
+    else hipLaunchKernelGGL(rms_norm_dx_kernel<float>, rows, dim3(256), 0, s, B, d, a);
   }
-  if (bf16) hipLaunchKernelGGL(rms_norm_dx_kernel<bf16_t>, rows, dim3(256), 0, s, B, d, a);
-  else hipLaunchKernelGGL(rms_norm_dx_kernel<float>, rows, dim3(256), 0, s, B, d, a);
+  if (a.dweight) hipLaunchKernelGGL(rms_norm_dw_finish_kernel, dim3((d + 63) / 64, L), dim3(64 * FINISH), 0, s, parts, d, a.part, a.dweight);
   return hipGetLastError();
 }
 
