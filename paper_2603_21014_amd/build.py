@@ -42,7 +42,7 @@ def vector_work_without_lanes(asm: str) -> list:
             kernel, empty = label.group(1), False
             continue
         if line.startswith("s_cbranch_execnz"):
-            empty = re.match(r"s_\w+ exec,", last) is not None
+            empty = re.match(r"s_(?!or_)\w+ exec,", last) is not None      # (an `or` only adds lanes: behind it the branch is always taken)
         elif empty:
             if re.match(r"s_\w+ exec,|s_\w+saveexec|s_branch|s_endpgm", line):
                 empty = False
