@@ -48,6 +48,24 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   return max(v, dpp_move<0x4E>(v));       // quad_perm [2,3,0,1]
 }
 
+// 4 x 4 words across the lanes of a quad: word j of lane i <-> word i of lane j
+__device__ __forceinline__ void quad_transpose(uint32_t (&w)[4], int i) {
+  const bool odd = i & 1, high = i & 2;
+  uint32_t a[4];
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {      // lanes i, i ^ 1
+    const uint32_t x = dpp_move<0xB1>(odd ? w[j] : w[j + 1]);
+    a[j] = odd ? x : w[j];
+    a[j + 1] = odd ? w[j + 1] : x;
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {         // lanes i, i ^ 2
+    const uint32_t x = dpp_move<0x4E>(high ? a[j] : a[j + 2]);
+    w[j] = high ? x : a[j];
+    w[j + 2] = high ? a[j + 2] : x;
+  }
+}
+
 // Eight consecutive elements as they come out of memory, and as floats
 template <typename TE> struct Eight;
 template <> struct Eight<float> {
@@ -83,7 +101,7 @@ __global__ __launch_bounds__(256) void mx4_quantise_kernel(int rows, int K, int 
   if (r >= rows) return;
   const TE* row = a + ((size_t)l * rows + r) * K;
   const float s = a_scale ? a_scale[(size_t)l * rows + r] : 1.f;
-  uint8_t* tile = codes + (((size_t)(l * panels + panel) * 4 + sub) * KS << 10) + lane * 4;
+  uint8_t* tile = codes + (((size_t)(l * panels + panel) * 4 + sub) * KS << 10) + part * 256 + (lane >> 2) * 16;
   uint8_t* sc = scales + ((size_t)(l * panels + panel) * KS << 8) + ((part * 16 + (lane >> 2)) << 2) + sub;
   Eight<TE> in[QUANTISE_STEPS][4];
 #pragma unroll
@@ -97,7 +115,7 @@ __global__ __launch_bounds__(256) void mx4_quantise_kernel(int rows, int K, int 
 #pragma unroll
   for (int t = 0; t < QUANTISE_STEPS; ++t) {
     if (ks0 + t >= KS) return;
-    uint32_t mine = 0;
+    uint32_t mine = 0, w[4];
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
       float x[8];
@@ -108,9 +126,11 @@ __global__ __launch_bounds__(256) void mx4_quantise_kernel(int rows, int K, int 
         top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
       }
       const uint32_t e = block_scale(quad_max(top));
-      *reinterpret_cast<uint32_t*>(tile + ((size_t)(ks0 + t) << 10) + kb * 256) = to_codes(x, e);
+      w[kb] = to_codes(x, e);
       mine = part == kb ? e : mine;
     }
+    quad_transpose(w, part);      // this lane: the four words of block `part`
+    *reinterpret_cast<u32x4*>(tile + ((size_t)(ks0 + t) << 10)) = u32x4{w[0], w[1], w[2], w[3]};
     sc[(size_t)(ks0 + t) << 8] = (uint8_t)mine;
   }
 }
@@ -148,27 +168,45 @@ __global__ __launch_bounds__(256) void mx4_quantise_transposed_kernel(int rows, 
   }
 }
 
-__device__ __forceinline__ float from_code(uint32_t c) {      // E2M1
-  const uint32_t m = c & 7u;
-  const float v = m < 2u ? 0.5f * m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
-  return c & 8u ? -v : v;
-}
+// 2^(s-127), NaN for s = 255
+__device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? 0x1p-127f : __uint_as_float(s << 23); }
 
+// The way back, cut as the way there: a wavefront takes 16 rows by one step; the lanes of a quad exchange the words of their four blocks, so that each
+// has eight consecutive elements of each block.
 template <typename T>
-__global__ __launch_bounds__(256) void mx4_dequantise_kernel(int rows, int K, int KS, Mx4 a, T* __restrict__ out) {
-  const int l = blockIdx.y, nb = (K + 7) / 8;
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;      // eight elements
-  const int r = (int)(i / nb), k = (int)(i % nb) * 8;
+__global__ __launch_bounds__(256) void mx4_dequantise_kernel(int rows, int K, int KS, int chunks, Mx4 a, T* __restrict__ out) {
+  const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6, panels = (rows + 63) >> 6, l = blockIdx.y;
+  const int panel = blockIdx.x / chunks, ks0 = (blockIdx.x - panel * chunks) * QUANTISE_STEPS;
+  const int part = lane & 3, r = panel * 64 + sub * 16 + (lane >> 2);
   if (r >= rows) return;
-  const int panels = (rows + 63) >> 6, kb = k >> 5;
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(a.codes + (((size_t)l * panels * 4 * KS) << 10) + code_offset(r, kb, KS) + ((k & 31) >> 1));
-  const uint32_t s = a.scales[(((size_t)l * panels * KS) << 8) + scale_offset(r, kb, KS)];
-  float v[8];
+  const uint8_t* tile = a.codes + (((size_t)(l * panels + panel) * 4 + sub) * KS << 10) + part * 256 + (lane >> 2) * 16;
+  const uint8_t* sc = a.scales + ((size_t)(l * panels + panel) * KS << 8) + ((part * 16 + (lane >> 2)) << 2) + sub;
+  T* row = out + ((size_t)l * rows + r) * K;
+  u32x4 in[QUANTISE_STEPS];
+  uint32_t mine[QUANTISE_STEPS];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = s == 255u ? __uint_as_float(0x7fc00000u) : __builtin_amdgcn_ldexpf(from_code(w >> (4 * j)), (int)s - 127);
-  T* o = out + ((size_t)l * rows + r) * K + k;
-  Elem<T>::store4(o, make_float4(v[0], v[1], v[2], v[3]));
-  Elem<T>::store4(o + 4, make_float4(v[4], v[5], v[6], v[7]));
+  for (int t = 0; t < QUANTISE_STEPS; ++t) {
+    const int ks = min(ks0 + t, KS - 1);
+    in[t] = *reinterpret_cast<const u32x4*>(tile + ((size_t)ks << 10));
+    mine[t] = sc[(size_t)ks << 8];
+  }
+#pragma unroll
+  for (int t = 0; t < QUANTISE_STEPS; ++t) {
+    uint32_t w[4] = {in[t][0], in[t][1], in[t][2], in[t][3]};
+    quad_transpose(w, part);
+    const float f = scale_value(mine[t]);
+    const float scale[4] = {__uint_as_float(dpp_move<0x00>(__float_as_uint(f))), __uint_as_float(dpp_move<0x55>(__float_as_uint(f))),
+                            __uint_as_float(dpp_move<0xAA>(__float_as_uint(f))), __uint_as_float(dpp_move<0xFF>(__float_as_uint(f)))};
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      const int k = (ks0 + t) * 128 + kb * 32 + part * 8;
+      if (k >= K) continue;
+      const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[kb], 1.0f, 0), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[kb], 1.0f, 1);
+      const auto z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[kb], 1.0f, 2), u = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[kb], 1.0f, 3);
+      Elem<T>::store4(row + k, make_float4(x[0] * scale[kb], x[1] * scale[kb], y[0] * scale[kb], y[1] * scale[kb]));
+      Elem<T>::store4(row + k + 4, make_float4(z[0] * scale[kb], z[1] * scale[kb], u[0] * scale[kb], u[1] * scale[kb]));
+    }
+  }
 }
 
 // ---- product -------------------------------------------------------------------------------------------------------
@@ -542,9 +580,10 @@ hipError_t launch_mx4_quantise(hipStream_t s, bool bf16, bool int8, bool transpo
 }
 
 hipError_t launch_mx4_dequantise(hipStream_t s, bool bf16, int L, int rows, int K, Mx4 a, void* out) {
-  const dim3 grid((uint32_t)(((size_t)rows * ((K + 7) / 8) + 255) / 256), L), wg(256);
-  if (bf16) hipLaunchKernelGGL(mx4_dequantise_kernel<bf16_t>, grid, wg, 0, s, rows, K, mx4_steps(K), a, (bf16_t*)out);
-  else hipLaunchKernelGGL(mx4_dequantise_kernel<float>, grid, wg, 0, s, rows, K, mx4_steps(K), a, (float*)out);
+  const int KS = mx4_steps(K), chunks = (KS + QUANTISE_STEPS - 1) / QUANTISE_STEPS;
+  const dim3 grid(mx4_panels(rows) * chunks, L), wg(256);
+  if (bf16) hipLaunchKernelGGL(mx4_dequantise_kernel<bf16_t>, grid, wg, 0, s, rows, K, KS, chunks, a, (bf16_t*)out);
+  else hipLaunchKernelGGL(mx4_dequantise_kernel<float>, grid, wg, 0, s, rows, K, KS, chunks, a, (float*)out);
   return hipGetLastError();
 }
 

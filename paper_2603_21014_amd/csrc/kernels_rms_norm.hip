@@ -20,6 +20,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 constexpr float ROW_IS_ZERO = 0x1p-100f;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Vec16 { static constexpr int N = 16 / sizeof(T); };      // elements in 16 bytes
 __device__ __forceinline__ void widen16(u32x4 r, float (&f)[8]) {
 #pragma unroll
@@ -34,6 +35,17 @@ __device__ __forceinline__ u32x4 narrow16(const float (&f)[8]) {
 }
 __device__ __forceinline__ u32x4 narrow16(const float (&f)[4]) {
   return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+}
+
+// 16, 8 or 4 bytes, STREAM: past the caches (see streams())
+template <bool STREAM, typename V> __device__ __forceinline__ V take(const void* p) {
+  const V* q = static_cast<const V*>(p);
+  return STREAM ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool STREAM, typename V> __device__ __forceinline__ void give(void* p, V v) {
+  V* q = static_cast<V*>(p);
+  if (STREAM) __builtin_nontemporal_store(v, q);
+  else *q = v;
 }
 
 // What the codes and the scale of a row follow from
@@ -54,7 +66,7 @@ __device__ __forceinline__ uint32_t code(float t, const RowScale& r) { return (u
 // bytes per lane, so that it is read once: the sum of squares and the largest |h weight| come from the same pass, and the codes
 // 127 y / max|y| need no second one because rstd cancels in them.  The weights stay in registers over the rows of a wavefront (they are
 // four bytes where a bf16 element is two).
-template <typename T, int NV, int W>
+template <typename T, int NV, int W, bool STREAM>
 __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_each, RmsNormArgs a) {
   constexpr int N = Vec16<T>::N;
   __shared__ float sums[2][4];
@@ -81,8 +93,8 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
     for (int v = 0; v < NV; ++v) {
       raw[v] = add[v] = u32x4{0u, 0u, 0u, 0u};
       if (e[v] < d) {
-        raw[v] = *reinterpret_cast<const u32x4*>(x + e[v]);
-        if (a.residual) add[v] = *reinterpret_cast<const u32x4*>(res + e[v]);
+        raw[v] = take<STREAM, u32x4>(x + e[v]);
+        if (a.residual) add[v] = take<STREAM, u32x4>(res + e[v]);
       }
     }
     float t[NV][N], s = 0.f;
@@ -97,7 +109,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
         for (int i = 0; i < N; ++i) h[i] += r[i];
         raw[v] = narrow16(h);      // the norm is that of the stored sum, as a model that reads it again would have it
         widen16(raw[v], h);
-        if (e[v] < d) *reinterpret_cast<u32x4*>(static_cast<T*>(a.h) + o + e[v]) = raw[v];
+        if (e[v] < d) give<STREAM>(static_cast<T*>(a.h) + o + e[v], raw[v]);
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -127,14 +139,14 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
         float y[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) y[i] = t[v][i] * r.rstd;
-        *reinterpret_cast<u32x4*>(static_cast<T*>(a.y) + o + e[v]) = narrow16(y);
+        give<STREAM>(static_cast<T*>(a.y) + o + e[v], narrow16(y));
       }
       if (a.q) {
         uint32_t c[N / 4];
 #pragma unroll
         for (int i = 0; i < N; i += 4) c[i / 4] = code(t[v][i], r) | code(t[v][i + 1], r) << 8 | code(t[v][i + 2], r) << 16 | code(t[v][i + 3], r) << 24;
-        if (N == 8) *reinterpret_cast<uint2*>(a.q + o + e[v]) = make_uint2(c[0], c[N / 4 - 1]);
-        else *reinterpret_cast<uint32_t*>(a.q + o + e[v]) = c[0];
+        if (N == 8) give<STREAM>(a.q + o + e[v], u32x2{c[0], c[N / 4 - 1]});
+        else give<STREAM>(a.q + o + e[v], c[0]);
       }
     }
   }
@@ -189,7 +201,7 @@ __global__ __launch_bounds__(256) void rms_norm_wide_kernel(int B, int d, RmsNor
 //
 // The same arrangement: h, dy (and dh) of a row are read once, for dx and for the row's share of dweight, which the lanes add up in
 // registers over all rows of their wavefront.  A workgroup leaves one partial sum of dweight, a second kernel adds those in order.
-template <typename T, int NV, int W>
+template <typename T, int NV, int W, bool STREAM>
 __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, int rows_each, RmsNormBackwardArgs a) {
   constexpr int N = Vec16<T>::N;
   __shared__ float sums[2][4];
@@ -216,9 +228,9 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
     for (int v = 0; v < NV; ++v) {
       rh[v] = rg[v] = re[v] = u32x4{0u, 0u, 0u, 0u};
       if (e[v] < d) {
-        rh[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.h) + o + e[v]);
-        rg[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.dy) + o + e[v]);
-        if (a.dh) re[v] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.dh) + o + e[v]);
+        rh[v] = take<STREAM, u32x4>(static_cast<const T*>(a.h) + o + e[v]);
+        rg[v] = take<STREAM, u32x4>(static_cast<const T*>(a.dy) + o + e[v]);
+        if (a.dh) re[v] = take<STREAM, u32x4>(static_cast<const T*>(a.dh) + o + e[v]);
       }
     }
     const float r = a.rstd[row];
@@ -251,7 +263,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
       widen16(re[v], x);
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] = fmaf(r, w[v][i] * g[i], fmaf(-c, h[i], x[i]));
-      if (e[v] < d) *reinterpret_cast<u32x4*>(static_cast<T*>(a.dx) + o + e[v]) = narrow16(x);
+      if (e[v] < d) give<STREAM>(static_cast<T*>(a.dx) + o + e[v], narrow16(x));
     }
   }
   if (!a.dweight) return;
@@ -368,15 +380,24 @@ inline int rows_each(int L, int B, int waves, int most) {
 
 }  // namespace
 
-#define ROW_KERNELS(KERNEL, T)                                                                                                      \
+#define ROW_KERNELS(KERNEL, T, STREAM)                                                                                              \
   do {                                                                                                                              \
     if (cut.waves == 1) {                                                                                                           \
-      if (cut.pieces == 1) hipLaunchKernelGGL((KERNEL<T, 1, 1>), grid, dim3(256), 0, s, B, d, each, a);                             \
-      else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 1>), grid, dim3(256), 0, s, B, d, each, a);                        \
-      else hipLaunchKernelGGL((KERNEL<T, 4, 1>), grid, dim3(256), 0, s, B, d, each, a);                                             \
-    } else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 4>), grid, dim3(256), 0, s, B, d, each, a);                        \
-    else hipLaunchKernelGGL((KERNEL<T, 4, 4>), grid, dim3(256), 0, s, B, d, each, a);                                               \
+      if (cut.pieces == 1) hipLaunchKernelGGL((KERNEL<T, 1, 1, STREAM>), grid, dim3(256), 0, s, B, d, each, a);                     \
+      else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 1, STREAM>), grid, dim3(256), 0, s, B, d, each, a);                \
+      else hipLaunchKernelGGL((KERNEL<T, 4, 1, STREAM>), grid, dim3(256), 0, s, B, d, each, a);                                     \
+    } else if (cut.pieces == 2) hipLaunchKernelGGL((KERNEL<T, 2, 4, STREAM>), grid, dim3(256), 0, s, B, d, each, a);                \
+    else hipLaunchKernelGGL((KERNEL<T, 4, 4, STREAM>), grid, dim3(256), 0, s, B, d, each, a);                                       \
   } while (0)
+#define ROW_KERNELS_T(KERNEL, bytes)                                                                                                \
+  do {                                                                                                                              \
+    if (bf16 && streams(bytes)) ROW_KERNELS(KERNEL, bf16_t, true);                                                                  \
+    else if (bf16) ROW_KERNELS(KERNEL, bf16_t, false);                                                                              \
+    else if (streams(bytes)) ROW_KERNELS(KERNEL, float, true);                                                                      \
+    else ROW_KERNELS(KERNEL, float, false);                                                                                         \
+  } while (0)
+// Streaming accesses where a call touches more than the Infinity Cache (256 MB) holds.
+static bool streams(double bytes) { return bytes > 256e6; }
 
 hipError_t launch_rms_norm(hipStream_t s, bool bf16, int L, int B, int d, const RmsNormArgs& a) {
   const RowCut cut = row_cut(bf16, d);
@@ -388,8 +409,8 @@ hipError_t launch_rms_norm(hipStream_t s, bool bf16, int L, int B, int d, const 
   }
   const int each = rows_each(L, B, cut.waves, 8), per = each * (cut.waves == 1 ? 4 : 1);
   const dim3 grid((B + per - 1) / per, L);
-  if (bf16) ROW_KERNELS(rms_norm_kernel, bf16_t);
-  else ROW_KERNELS(rms_norm_kernel, float);
+  const double n = (double)L * B * d, e = bf16 ? 2 : 4;
+  ROW_KERNELS_T(rms_norm_kernel, n * (e * (1 + (a.residual ? 2 : 0) + (a.y ? 1 : 0)) + (a.q ? 1 : 0)));
   return hipGetLastError();
 }
 
@@ -411,8 +432,7 @@ hipError_t launch_rms_norm_backward(hipStream_t s, bool bf16, int L, int B, int 
   if (cut.pieces) {
     const int each = rows_each(L, B, cut.waves, B);
     const dim3 grid(parts, L);
-    if (bf16) ROW_KERNELS(rms_norm_backward_kernel, bf16_t);
-    else ROW_KERNELS(rms_norm_backward_kernel, float);
+    ROW_KERNELS_T(rms_norm_backward_kernel, (double)L * B * d * (bf16 ? 2 : 4) * (a.dh ? 4 : 3));
   } else {
     const dim3 rows((uint32_t)((size_t)L * B)), cols((d + 255) / 256, parts, L);
     if (a.dweight) {      // before dx, which may overwrite dy
