@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) void mx4_product_few_kernel(ProductArgs p) {
     sa[buf] = as.lanes4(lane, (uint32_t)ks << 8);
   };
   auto compute = [&](int buf) {
-    const uint32_t s = MT == 4 ? sa[buf] : sa[buf] >> (8 * ((token0 >> 4) & 3));
+    const uint32_t s = sa[buf] >> (8 * ((token0 >> 4) & 3));      // (MT = 2: token0 is a multiple of 32)
 #pragma unroll
     for (int i = 0; i < MT; ++i) mfma4(i, fb[buf], fa[buf][i], s, acc[i]);
   };
@@ -549,15 +549,19 @@ __global__ __launch_bounds__(256) void mx4_product_few_kernel(ProductArgs p) {
 
 template <typename T, bool THETA>
 hipError_t launch_product(hipStream_t s, int L, const ProductArgs& p) {
-  const int panels_n = (p.N + 63) / 64;
-  if (p.M <= 64) {
-    const dim3 wg(256);
-    if (p.M <= 16) hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 1>), dim3(panels_n, 1, L), wg, 0, s, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 2>), dim3(panels_n, 1, L), wg, 0, s, p);
-    else hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 4>), dim3(panels_n, 1, L), wg, 0, s, p);
+  const int panels_n = (p.N + 63) / 64, tiles_m = (p.M + PT * 16 - 1) / (PT * 16), tiles_n = (panels_n + 3) / 4;
+  // The kernel for few tokens: up to 32 of them, and where tiles are too few for the chip.  us with it and with the other one (L, M, N, K):
+  // 16, 1, 8192, 2048 22.0 / 22.4; 1, 64, 8192, 2048 (32 tiles) 4.9 / 11.2; 1, 300, 2048, 8192 (24) 11.1 / 32.7; 4, 128, 6144, 768 (96) 6.5 / 8.3;
+  // 1, 512, 8192, 2048 (128) 12.2 / 13.0; 1, 768, 8192, 2048 (192) 17.2 / 13.6; 8, 128, 8192, 2048 (256) 22.3 / 14.9; 12, 64, 6144, 768 (288) 8.7 / 10.2;
+  // 16, 48, 8192, 2048 (512) 25.5 / 24.5.  Two tiles of tokens instead of one at 17 to 32 tokens: 12 layers of 6144, K = 768 6.2 and 6.6.
+  if (p.M <= 16) {
+    hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 1>), dim3(panels_n, 1, L), dim3(256), 0, s, p);
     return hipGetLastError();
   }
-  const int tiles_m = (p.M + PT * 16 - 1) / (PT * 16), tiles_n = (panels_n + 3) / 4;
+  if (p.M <= 32 || (double)L * tiles_m * tiles_n < 160.0) {
+    hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 2>), dim3(panels_n, (p.M + 31) / 32, L), dim3(256), 0, s, p);
+    return hipGetLastError();
+  }
   const TileOrder order(L, tiles_m, tiles_n);
   const uint32_t grid = order.tiles >= WORKGROUPS ? WORKGROUPS : (order.tiles + 7) / 8 * 8;
   hipLaunchKernelGGL((mx4_product_kernel<T, THETA>), dim3(grid), dim3(256), 0, s, p, order);

@@ -16,7 +16,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return v;
 }
 
-// Rows whose largest |h w| is below this count as all-zero (127 / max must not overflow).
+// Rows whose largest |h w| is below this count as all-zero (1 / max must not overflow).
 constexpr float ROW_IS_ZERO = 0x1p-100f;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -56,7 +56,7 @@ __device__ __forceinline__ RowScale row_scale(float sum, uint32_t top, float eps
   const float amax = __uint_as_float(top);
   const bool zero = amax < ROW_IS_ZERO;
   r.broken = top >= 0x7f800000u;
-  r.k = r.broken || zero ? 0.f : 127.0f / amax;
+  r.k = r.broken || zero ? 0.f : 1.0f / amax * 127.0f;
   r.scale = r.broken ? __uint_as_float(0x7fc00000u) : zero ? 1.f : amax * r.rstd / 127.0f;
   return r;
 }
