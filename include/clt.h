@@ -330,7 +330,7 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
  *   codes   [L][4 RP][KS][4 blocks of 32][16 rows][16 bytes]: element k of a block in byte k / 2, even k in the low half
  *   scales  [L][RP][KS][4 blocks of 32][16 rows][4]: row r of a panel at [r % 16][r / 16]
  * The elements of a row from K up to 128 KS are zeros.  Rows beyond `rows` are room that is never written and whose contents
- * reach no result.  L <= 65535, rows <= 2^20, K <= 2^24 a positive multiple of 8, rows * KS < 2^28. */
+ * reach no result.  L <= 65535, rows <= 2^20, K <= 2^22 a positive multiple of 8, rows * KS < 2^28. */
 int clt_mx4_bytes(int32_t L, int32_t rows, int32_t K, size_t* codes_bytes, size_t* scales_bytes);
 
 /* Packs a: [L][rows][K] of T or, with CLT_INPUT_INT8_ROWSCALE (dtype bf16), int8 codes times a_scale [L][rows]; with

@@ -914,8 +914,8 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
 
 // (the sizes that the kernels' 32-bit block counts and grids hold)
 static int check_packed(const char* who, int32_t L, int32_t rows, int32_t K) {
-  if (L < 1 || L > 65535 || rows < 1 || rows > 1 << 20 || K < 8 || K > 1 << 24 || (K % 8) || (int64_t)rows * mx4_steps(K) >= (int64_t)1 << 28)
-    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d rows=%d K=%d (need 1<=L<=65535, 1<=rows<=2^20, K<=2^24 a positive multiple of 8, rows*ceil(K/128)<2^28)",
+  if (L < 1 || L > 65535 || rows < 1 || rows > 1 << 20 || K < 8 || K > 1 << 22 || (K % 8) || (int64_t)rows * mx4_steps(K) >= (int64_t)1 << 28)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d rows=%d K=%d (need 1<=L<=65535, 1<=rows<=2^20, K<=2^22 a positive multiple of 8, rows*ceil(K/128)<2^28)",
          who, L, rows, K);
   return CLT_OK;
 }

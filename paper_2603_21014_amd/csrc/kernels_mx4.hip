@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256) void mx4_dequantise_kernel(int rows, int K, in
 // operand, those of A (tokens) its second, so a lane's four results are four consecutive features of one token.
 
 // Loads of 16 or 4 bytes per lane, consecutive lanes, from `offset` bytes on: through buffer descriptors, which keep everything but
-// the lane's own offset (one register for all loads) in scalar registers.  A panel of K <= 2^24 is at most 2^29 bytes.
+// the lane's own offset (one register for all loads) in scalar registers.  A panel of K <= 2^22 is at most 2^27 bytes.
 struct Source {
   __amdgpu_buffer_rsrc_t d;
   __device__ __forceinline__ Source(const uint8_t* base) : d(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, 0x7fffffff, 0x00027000)) {}

@@ -143,10 +143,31 @@ def test_product(dtype, L, M, N, K):
         out.check()
 
 
+# Where tiles of 128 tokens by 256 features are enough for the chip (160 and more): one step and many, fewer tiles than workgroups, as many, and
+# several to each; tokens, features and tile groups that end early
+TILED = [(160, 33, 8, 8), (83, 130, 264, 128), (300, 129, 264, 136), (1, 2600, 2056, 264), (2, 1700, 4104, 392), (1, 5000, 4104, 136), (20, 1000, 264, 4104), (700, 65, 40, 256),
+         (5, 1030, 1288, 640), (512, 128, 256, 128), (1, 20488, 24, 384)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,M,N,K", TILED)
+def test_product_of_many_tiles(dtype, L, M, N, K):
+    from paper_2603_21014_amd import binding as B
+    assert M > 32 and L * -(-M // 128) * -(-N // 256) >= 160
+    packed, va, vw = operands(B, L, M, N, K)
+    bias, theta = 0.1 * normal(30, L, N), 0.2 + 0.1 * normal(31, L, N)
+    for b, t in ((None, None), (bias, theta), (bias, None), (None, theta))[:2 if L * M * N > 1 << 22 else 4]:
+        out = Guarded((L, M, N), T[dtype])
+        B.clt_mx4_product(*packed, out.t, K, bias=None if b is None else b.to(DEV), theta=None if t is None else t.to(DEV))
+        torch.cuda.synchronize()
+        check_product(out.t, va, vw, b, t, dtype)
+        out.check()
+
+
 def test_product_of_broken_blocks():
     """A block with a NaN makes its row (or column) NaN and no other; with a threshold NaN is not above it."""
     from paper_2603_21014_amd import binding as B
-    for M in (3, 150):
+    for M in (3, 150, 20600):
         L, N, K = 1, 72, 264
         a, w = matrix(L, M, K, "bf16"), normal(9, L, N, K)
         a[0, 2, 200], w[0, 11, 3] = float("nan"), float("inf")
@@ -166,22 +187,22 @@ def test_product_of_broken_blocks():
 def test_product_of_exact_numbers_is_exact():
     """Small whole numbers with one scale: every partial sum is a number that fp32 holds, so the order of the sum cannot matter."""
     from paper_2603_21014_amd import binding as B
-    L, M, N, K = 2, 300, 264, 1000
-    g = torch.Generator().manual_seed(3)
-    a, w = (torch.randint(-4, 5, s, generator=g).float() for s in ((L, M, K), (L, N, K)))
-    a[:, :, ::32], w[:, :, ::32] = 4.0, -4.0
-    (ac, as_), (bc, bs) = B.mx4_empty(L, M, K, DEV), B.mx4_empty(L, N, K, DEV)
-    B.clt_mx4_quantise(a.to(DEV), ac, as_)
-    B.clt_mx4_quantise(w.to(DEV), bc, bs)
-    out = torch.empty(L, M, N, device=DEV)
-    B.clt_mx4_product(ac, as_, bc, bs, out, K)
-    assert torch.equal(out.cpu().double(), torch.matmul(a.double(), w.double().transpose(1, 2)))
+    for L, M, N, K in ((2, 16, 264, 1000), (2, 300, 264, 1000), (50, 300, 264, 1000), (7, 1100, 1032, 520)):
+        g = torch.Generator().manual_seed(3)
+        a, w = (torch.randint(-4, 5, s, generator=g).float() for s in ((L, M, K), (L, N, K)))
+        a[:, :, ::32], w[:, :, ::32] = 4.0, -4.0
+        (ac, as_), (bc, bs) = B.mx4_empty(L, M, K, DEV), B.mx4_empty(L, N, K, DEV)
+        B.clt_mx4_quantise(a.to(DEV), ac, as_)
+        B.clt_mx4_quantise(w.to(DEV), bc, bs)
+        out = torch.empty(L, M, N, device=DEV)
+        B.clt_mx4_product(ac, as_, bc, bs, out, K)
+        assert torch.equal(out.cpu().double(), torch.matmul(a.double(), w.double().transpose(1, 2).contiguous()))
 
 
 def test_streams_and_graphs():
     from paper_2603_21014_amd import binding as B
-    for M in (1, 40, 300):
-        L, N, K = 2, 520, 776
+    for L, M in ((2, 1), (2, 40), (2, 300), (30, 200), (90, 200)):
+        N, K = 520, 776
         x, w = matrix(L, M, K, "bf16").to(DEV), (normal(8, L, K, N) / K ** 0.5).to(DEV)
         (ac, as_), (bc, bs) = B.mx4_empty(L, M, K, DEV), B.mx4_empty(L, N, K, DEV)
         out = torch.empty(L, M, N, dtype=torch.bfloat16, device=DEV)
