@@ -267,7 +267,8 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
  * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
  * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN gets codes 0 and a NaN as its scale.
- * Except for h, an output must not overlap an input.  1 <= L <= 128, B >= 1, L B < 2^30, d a positive multiple of 8, eps > 0. */
+ * Except for h, an output must not overlap an input.  1 <= L <= 128, B >= 1, L B < 2^30, d <= 2^20 a positive multiple of 8,
+ * eps > 0. */
 int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
                  const float* weight, float eps, void* h, void* y, int8_t* q, float* q_scale, float* rstd);
 
@@ -283,7 +284,7 @@ int clt_rms_norm_backward(void* stream, int32_t L, int32_t B, int32_t d, int32_t
                           const float* rstd, const void* dy, const void* dh, void* dx, float* dweight, void* workspace,
                           size_t workspace_bytes);
 
-/* One tensor of clt_adamw_step, n >= 0 elements, contiguous.  Moments in 32 bits: m, v float, m_scale and v_scale NULL.
+/* One tensor of clt_adamw_step, 0 <= n <= 2^34 elements, contiguous.  Moments in 32 bits: m, v float, m_scale and v_scale NULL.
  * Moments in 8 bits, in blocks of CLT_ADAMW_BLOCK consecutive elements (the last one may be shorter), each with a
  * power of two 2^(s-127) of its own, s one byte in m_scale / v_scale (ceil(n / CLT_ADAMW_BLOCK) bytes each; the OCP
  * formats E4M3 for m, E5M2 for v, E8M0 for the scales): value = element * 2^(s-127).  All bytes 0 is a state of
@@ -314,8 +315,9 @@ typedef struct clt_adamw_tensor {
  * that rounding to nearest would never let it move; and because the scales are powers of two, a value that stays
  * keeps its neighbours from step to step, and the noise stays near the square root of (step x drift).  The random
  * bits are a function of (seed, t, position in the list, element), so a step can be repeated bit for bit; a v' above
- * zero never rounds to zero.  t >= 1 is the step count, lr >= 0, 0 <= beta < 1, eps > 0 (doubles, so that 1 - beta and
- * the bias corrections are formed before they are rounded to float).  Tensors must not overlap. */
+ * zero never rounds to zero.  t >= 1 is the step count, lr >= 0, 0 <= beta < 1, eps >= 2^-126 (doubles, so that 1 - beta
+ * and the bias corrections are formed before they are rounded to float); a captured step keeps those of its capture.
+ * What the step writes must not overlap anything else of the list: a tensor appears in it once. */
 int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tensors, int64_t t, double lr, double beta1,
                    double beta2, double eps, uint64_t seed);
 

@@ -375,7 +375,8 @@ ADAMW_BLOCK = 128
 class AdamWTensor:
     """One tensor of clt_adamw_step: parameters p, gradient g (each float32 or bfloat16), moments m and v: float32, or uint8
     with the block scales m_scale and v_scale (uint8, one per 128 elements); master: float32 copy of p.  Any shape,
-    contiguous; p, g, m, v and master have the same number of elements."""
+    contiguous; p, g, m, v and master have the same number of elements.  It stands for the tensors' present memory: one that is
+    given other memory (a new p.data, a new p.grad) needs a new AdamWTensor."""
 
     def __init__(self, p, g, m, v, m_scale=None, v_scale=None, master=None, weight_decay=0.0):
         dev = _device_of(p, "p")
@@ -394,7 +395,9 @@ class AdamWTensor:
         _may(m_scale, dev, blocks, torch.uint8, "m_scale")
         _may(v_scale, dev, blocks, torch.uint8, "v_scale")
         self.device = dev
-        self.tensors = (p, g, m, v, m_scale, v_scale, master)      # kept alive
+        self.tensors = (p, g, m, v, m_scale, v_scale, master)
+        # kept alive, whatever the tensors are given afterwards: the step works on this memory
+        self.storages = tuple(t.untyped_storage() for t in self.tensors if t is not None)
         self.c = clt_adamw_tensor(*(None if t is None else t.data_ptr() for t in self.tensors), n, _TYPES[p.dtype], _TYPES[g.dtype],
                                   8 if eight else 32, float(weight_decay))
 
@@ -412,6 +415,14 @@ class AdamW:
         self.device = self.tensors[0].device if self.tensors else None
         if any(t.device != self.device for t in self.tensors):
             raise ValueError("the tensors are on different devices")
+        # what a step writes (every tensor but the gradients) overlaps nothing else, such as a weight that is in the list twice
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k != 1) for x in self.tensors for k, t in enumerate(x.tensors)
+                       if t is not None and t.numel())
+        end, end_written = 0, 0      # of all spans so far, of the written ones
+        for a, b, written in spans:
+            if a < (end if written else end_written):
+                raise ValueError("the tensors overlap in memory")
+            end, end_written = max(end, b), max(end_written, b if written else 0)
         self._array = (clt_adamw_tensor * max(1, len(self.tensors)))(*(t.c for t in self.tensors))
         self.scalars = (float(beta1), float(beta2), float(eps), int(seed))
 

@@ -824,8 +824,8 @@ int clt_adam_step(clt_handle* h, void* stream, int64_t t, float lr, const clt_te
   } while (0)
 
 static int check_rows(const char* who, int32_t L, int32_t B, int32_t d) {
-  if (L < 1 || L > 128 || B < 1 || d < 8 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 30)
-    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^30, d a positive multiple of 8)", who, L, B, d);
+  if (L < 1 || L > 128 || B < 1 || d < 8 || d > 1 << 20 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 30)
+    FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^30, d<=2^20 a positive multiple of 8)", who, L, B, d);
   return CLT_OK;
 }
 
@@ -875,11 +875,11 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
                    double beta2, double eps, uint64_t seed) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad list of tensors");
   if (t < 1) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: step count t must be >= 1");
-  if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f))
-    FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: need lr>=0, 0<=beta<1, eps>0");
+  if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 0x1p-126f))
+    FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: need lr>=0, 0<=beta<1, eps>=2^-126");
   for (int32_t i = 0; i < n_tensors; ++i) {
     const clt_adamw_tensor& q = tensors[i];
-    if (q.n < 0 || q.n > (int64_t)1 << 40) FAIL(CLT_ERR_SHAPE, "clt_adamw_step: tensor %d has n=%lld (need 0<=n<=2^40)", i, (long long)q.n);
+    if (q.n < 0 || q.n > (int64_t)1 << 34) FAIL(CLT_ERR_SHAPE, "clt_adamw_step: tensor %d has n=%lld (need 0<=n<=2^34)", i, (long long)q.n);
     if ((q.dtype != CLT_DTYPE_F32 && q.dtype != CLT_DTYPE_BF16) || (q.grad_dtype != CLT_DTYPE_F32 && q.grad_dtype != CLT_DTYPE_BF16) ||
         (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f))
       FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: bad dtype, grad_dtype, state_bits or weight_decay", i);
@@ -896,8 +896,8 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
   const uint32_t key_t = adamw_mix((uint32_t)((uint64_t)t >> 32)) ^ (uint32_t)t;
   for (int32_t i = 0; i < n_tensors; ++i) {
     const clt_adamw_tensor& q = tensors[i];
-    const uint32_t chunks = (uint32_t)((q.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK);      // at most 2^29
-    if (list.count == ADAMW_TENSORS || (uint64_t)list.chunks + chunks >= (uint64_t)1 << 31) {
+    const uint32_t chunks = (uint32_t)((q.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK);      // at most 2^23
+    if (list.count == ADAMW_TENSORS || list.chunks + chunks >= 1u << 24) {      // (a grid holds 2^32 threads)
       LAUNCH(launch_adamw(static_cast<hipStream_t>(stream), list));
       list.count = 0; list.chunks = 0;
     }

@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
       if (e[v] < d) *reinterpret_cast<float4*>(out + e[v] + i) = make_float4(dw[v][i], dw[v][i + 1], dw[v][i + 2], dw[v][i + 3]);
 }
 
-// Rows too wide for that.  dx: one workgroup per row, the row read twice; dweight: sums over DW_ROWS rows, a lane per column
+// Rows too wide for that.  dx: one workgroup per row, the row read twice; dweight: sums over dw_rows(B) rows, a lane per column
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_dx_kernel(int B, int d, RmsNormBackwardArgs a) {
   __shared__ float sums[4];
@@ -319,17 +319,17 @@ __global__ __launch_bounds__(256) void rms_norm_dx_kernel(int B, int d, RmsNormB
   }
 }
 
-constexpr int DW_ROWS = 32;      // rows of a partial sum
-inline int dw_blocks(int B) { return (B + DW_ROWS - 1) / DW_ROWS; }
+inline int dw_rows(int B) { return B <= 1 << 20 ? 32 : (B + 32767) / 32768; }      // rows of a partial sum (a grid has 65535 blocks along its second axis)
+inline int dw_blocks(int B) { return (B + dw_rows(B) - 1) / dw_rows(B); }
 
 // grid = (columns / 256, row blocks, layers)
 template <typename T>
-__global__ __launch_bounds__(256) void rms_norm_dw_kernel(int B, int d, RmsNormBackwardArgs a) {
+__global__ __launch_bounds__(256) void rms_norm_dw_kernel(int B, int d, int rows, RmsNormBackwardArgs a) {
   const int c = blockIdx.x * 256 + threadIdx.x, l = blockIdx.z;
   if (c >= d) return;
-  const int end = min(B, (int)(blockIdx.y + 1) * DW_ROWS);
+  const int end = min(B, (int)(blockIdx.y + 1) * rows);
   float s = 0.f;
-  for (int b = blockIdx.y * DW_ROWS; b < end; ++b) {
+  for (int b = blockIdx.y * rows; b < end; ++b) {
     const size_t row = (size_t)l * B + b;
     s = fmaf(Elem<T>::load(static_cast<const T*>(a.dy) + row * d + c) * a.rstd[row], Elem<T>::load(static_cast<const T*>(a.h) + row * d + c), s);
   }
@@ -407,7 +407,8 @@ hipError_t launch_rms_norm(hipStream_t s, bool bf16, int L, int B, int d, const 
     else hipLaunchKernelGGL(rms_norm_wide_kernel<float>, grid, dim3(256), 0, s, B, d, a);
     return hipGetLastError();
   }
-  const int each = rows_each(L, B, cut.waves, 8), per = each * (cut.waves == 1 ? 4 : 1);
+  // (8 rows that share the weights; more of them where the grid, of 2^32 threads at most, would not hold a wavefront for every eight)
+  const int each = rows_each(L, B, cut.waves, B <= 1 << 28 ? 8 : 32), per = each * (cut.waves == 1 ? 4 : 1);
   const dim3 grid((B + per - 1) / per, L);
   const double n = (double)L * B * d, e = bf16 ? 2 : 4;
   ROW_KERNELS_T(rms_norm_kernel, n * (e * (1 + (a.residual ? 2 : 0) + (a.y ? 1 : 0)) + (a.q ? 1 : 0)));
@@ -436,8 +437,8 @@ hipError_t launch_rms_norm_backward(hipStream_t s, bool bf16, int L, int B, int 
   } else {
     const dim3 rows((uint32_t)((size_t)L * B)), cols((d + 255) / 256, parts, L);
     if (a.dweight) {      // before dx, which may overwrite dy
-      if (bf16) hipLaunchKernelGGL(rms_norm_dw_kernel<bf16_t>, cols, dim3(256), 0, s, B, d, a);
-      else hipLaunchKernelGGL(rms_norm_dw_kernel<float>, cols, dim3(256), 0, s, B, d, a);
+      if (bf16) hipLaunchKernelGGL(rms_norm_dw_kernel<bf16_t>, cols, dim3(256), 0, s, B, d, dw_rows(B), a);
+      else hipLaunchKernelGGL(rms_norm_dw_kernel<float>, cols, dim3(256), 0, s, B, d, dw_rows(B), a);
     }
     if (bf16) hipLaunchKernelGGL(rms_norm_dx_kernel<bf16_t>, rows, dim3(256), 0, s, B, d, a);
     else hipLaunchKernelGGL(rms_norm_dx_kernel<float>, rows, dim3(256), 0, s, B, d, a);

@@ -218,5 +218,28 @@ def test_misaligned_and_foreign_tensors_are_refused():
         K.AdamWTensor(x[::2], x[::2].contiguous(), x[:65], x[:65])
     with pytest.raises(ValueError):
         K.AdamWTensor(x, x, x.to(torch.uint8), x.to(torch.uint8), x[:1].to(torch.uint8), x[:1].to(torch.uint8))
+    # a weight that is in the list twice, its moments apart; a gradient that a step would overwrite; one gradient for two weights is none
+    f = lambda n=64: torch.zeros(n, device=DEV)
+    p, g = f(), f()
+    for a, b in (((p, g, f(), f()), (p, g, f(), f())), ((p, g, f(), f()), (f(32), p[16:48], f(32), f(32))), ((p, p, f(), f()), None),
+                 ((x[:64], g, f(), f()), (x[60:124], g, f(), f())), ((p, g, x[:64], x[32:96]), None)):
+        with pytest.raises(ValueError, match="overlap"):
+            K.AdamW([K.AdamWTensor(*c) for c in (a, b) if c])
+    K.AdamW([K.AdamWTensor(p, g, f(), f()), K.AdamWTensor(x[:64], g, f(), x[64:128])])
     torch.cuda.synchronize()
     assert not x.any()
+
+
+def test_tensors_that_get_other_memory_leave_the_list_its_own():
+    from paper_2603_21014_amd import binding as K
+    p, g, m, v = (torch.ones(1000, device=DEV) for _ in range(4))
+    opt = K.AdamW([K.AdamWTensor(p, g, m, v)])
+    old = p.detach()
+    ptr = old.data_ptr()
+    p.data = torch.full((1000,), 7.0, device=DEV)
+    del old
+    other = [torch.full((1000,), 5.0, device=DEV) for _ in range(8)]      # (would take the freed memory)
+    assert all(t.data_ptr() != ptr for t in other)
+    opt.step(1, 1e-3)
+    torch.cuda.synchronize()
+    assert torch.all(p == 7.0) and all(torch.all(t == 5.0) for t in other)

@@ -70,6 +70,40 @@ def test_rms_norm_and_gradients_behind_2_to_the_32():
     assert np.all(np.abs(np64(dw) - want_dw) <= np.abs(np64(hg) * np64(hx) * np64(rstd[:, -70:])[..., None]).sum(1) * 78 * U)
 
 
+def test_rms_norm_of_very_many_rows():
+    """More rows than a grid has wavefronts for, eight each; and wide ones with more partial sums than a grid's second axis holds."""
+    from paper_2603_21014_amd import binding as K
+    B, d = (1 << 29) + 37, 8
+    x, w = torch.zeros(1, B, d, dtype=torch.bfloat16, device=DEV), 1 + 0.1 * normal(1, 1, d)
+    hx = normal(2, 1, 100, d).bfloat16()
+    x[:, -100:] = hx.to(DEV)
+    y, rstd = torch.full_like(x, 3.0), torch.empty(1, B, device=DEV)
+    K.clt_rms_norm(x, w.to(DEV), 1e-5, y=y, rstd=rstd)
+    _, want_r, want_y = R.rms_norm(np32(hx), np64(w), 1e-5)
+    assert np.all(np.abs(np64(y[:, -100:]) - want_y) <= np.abs(want_y) * (HALF["bf16"] + 25 * U) * (1 + 2.0 ** -7))
+    assert not y[:, :-100].any()
+    ws = torch.empty(K.clt_rms_norm_backward_workspace_bytes(1, B, d), dtype=torch.uint8, device=DEV)
+    dw = torch.empty(1, d, device=DEV)
+    K.clt_rms_norm_backward(x, w.to(DEV), rstd, x, y, dw, ws)
+    _, want_dw = R.rms_norm_backward(np32(hx), np64(w), np64(rstd[:, -100:]), np32(hx))
+    assert np.all(np.abs(np64(dw) - want_dw) <= (np64(hx) ** 2 * np64(rstd[:, -100:])[..., None]).sum(1) * 108 * U)
+    del x, y, rstd, ws
+    torch.cuda.empty_cache()
+    B, d = 65535 * 32 + 50, 4104
+    h, dy = torch.zeros(1, B, d, device=DEV), torch.zeros(1, B, d, device=DEV)
+    hx, hg, w = normal(3, 1, 40, d), normal(4, 1, 40, d), 1 + 0.1 * normal(5, 1, d)
+    h[:, -40:], dy[:, -40:] = hx.to(DEV), hg.to(DEV)
+    rstd = torch.ones(1, B, device=DEV)
+    ws = torch.empty(K.clt_rms_norm_backward_workspace_bytes(1, B, d), dtype=torch.uint8, device=DEV)
+    dw = torch.empty(1, d, device=DEV)
+    K.clt_rms_norm_backward(h, w.to(DEV), rstd, dy, dy, dw, ws)
+    want_dx, want_dw = R.rms_norm_backward(np32(hx), np64(w), np.ones((1, 40)), np32(hg))
+    assert np.all(np.abs(np64(dw) - want_dw) <= np.abs(np64(hg) * np64(hx)).sum(1) * 48 * U)
+    size = np.abs(np64(w) * np64(hg)) + np.abs(np64(hx)) * np.abs(np64(w) * np64(hg) * np64(hx)).mean(-1, keepdims=True)
+    assert np.all(np.abs(np64(dy[:, -40:]) - want_dx) <= U * np.abs(want_dx) + size * (d / 64 + 24) * 1.01 * U)
+    assert not dy[:, :-40].any()
+
+
 def test_mx4_behind_2_to_the_32():
     from paper_2603_21014_amd import binding as K
     # a packed operand of 2^32 + ... elements, rows along the contraction and transposed

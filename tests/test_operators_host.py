@@ -32,7 +32,7 @@ def test_rms_norm_refusals(K):
 
     def call(L=2, B=3, d=64, dtype=K.DTYPE_BF16, x=P, residual=None, weight=P, eps=1e-5, h=None, y=P, q=None, q_scale=None, rstd=None):
         return f(None, L, B, d, dtype, x, residual, weight, eps, h, y, q, q_scale, rstd)
-    for bad in (dict(L=0), dict(L=129), dict(B=0), dict(B=-1), dict(d=0), dict(d=12), dict(L=128, B=1 << 24)):
+    for bad in (dict(L=0), dict(L=129), dict(B=0), dict(B=-1), dict(d=0), dict(d=12), dict(d=(1 << 20) + 8), dict(L=128, B=1 << 24)):
         refused(K, -2, "shape", call(**bad))
     refused(K, -1, "dtype", call(dtype=2))
     for eps in (0.0, -1.0, float("nan")):
@@ -83,10 +83,10 @@ def test_adamw_refusals(K):
     refused(K, -1, "list", call(count=-1))
     assert K._lib.clt_adamw_step(None, 1, None, 1, 1e-3, 0.9, 0.999, 1e-8, 0) == -1
     refused(K, -1, "step count", call(tensor(), t=0))
-    for bad in (dict(lr=-1.0), dict(lr=float("nan")), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(eps=0.0), dict(eps=1e-60)):
+    for bad in (dict(lr=-1.0), dict(lr=float("nan")), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39)):
         refused(K, -1, "scalar", call(tensor(), **bad))
     refused(K, -2, "tensor 1", call(tensor(**good8), tensor(n=-1)))
-    refused(K, -2, "tensor 0", call(tensor(n=(1 << 40) + 1)))
+    refused(K, -2, "tensor 0", call(tensor(n=(1 << 34) + 1)))
     for bad in (dict(dtype=2), dict(grad_dtype=2), dict(bits=16), dict(decay=-0.1), dict(decay=float("nan"))):
         refused(K, -1, "tensor 1", call(tensor(), tensor(**bad)))
     for name in ("p", "g", "m", "v"):
@@ -103,7 +103,7 @@ def test_adamw_refusals(K):
 
 def test_mx4_refusals(K):
     assert K.clt_mx4_bytes(3, 65, 136) == (3 * 2 * 2 * 4096, 3 * 2 * 2 * 256)
-    for bad in ((0, 8, 64), (1, 0, 64), (1, 8, 0), (1, 8, 12), (65536, 8, 64), (1, (1 << 20) + 1, 64), (1, 1 << 20, 1 << 16)):
+    for bad in ((0, 8, 64), (1, 0, 64), (1, 8, 0), (1, 8, 12), (65536, 8, 64), (1, (1 << 20) + 1, 64), (1, 1 << 20, 1 << 16), (1, 8, (1 << 22) + 8)):
         with pytest.raises(K.CLTError) as e:
             K.clt_mx4_bytes(*bad)
         assert e.value.code == -2
