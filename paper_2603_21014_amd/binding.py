@@ -108,7 +108,8 @@ def _check(rc, handle=None):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # (by its pointer: making a torch.cuda.Stream object of it takes 2.7 us of a call's 9)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _ptr(t, shape, dtype, name, optional=False):
