@@ -9,6 +9,7 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // Byte offsets of block `kb` (32 elements, counted from the start of the row) of row r in a packed matrix of KS steps
@@ -28,10 +29,10 @@ __device__ __forceinline__ uint32_t block_scale(uint32_t top) {
 // for s = 0 is the denormal 2^-127: such blocks are multiplied by 2^64 first and converted with 2^(s-127+64).
 __device__ __forceinline__ uint32_t to_codes(const float* x, uint32_t s) {
   const bool small = s < 64u;
-  const float scale = __uint_as_float((small ? s + 64u : s) << 23);
+  const float scale = __uint_as_float((small ? s + 64u : s) << 23), up = small ? 0x1p64f : 1.f;
   float y[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = small ? x[j] * 0x1p64f : x[j];
+  for (int j = 0; j < 8; ++j) y[j] = x[j] * up;
   uint32_t w = 0;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
@@ -375,16 +376,26 @@ struct TileOrder {
 struct Cursor {
   uint32_t t; int ks, l, tm, panel; bool ok;
 };
-template <typename T, bool THETA>
+//
+// Results leave a wavefront in one of two ways.  Directly: at the end of a tile its 16 or 32 stores are issued at once, and because loads and
+// stores are counted in order, the first operands of the next tile are waited for together with all of them.  STAGED (bf16): the results are put into
+// LDS (rounded, 14 KB a wavefront, and 2 KB in the stage that is free at that moment, which makes 80 KB for a workgroup), and every step of the next tile
+// reads one sixteen tokens' worth back as whole lines and stores it behind its loads, so that a store has a step's time; bias and threshold are fetched with the
+// tile's first features.  The stores go through a buffer descriptor that ends with the tile's last token: what lies beyond is not written, without a branch.
+// (The place is in the descriptor's base: a 16-byte store whose offset was in a scalar register has lost its first word to the next
+// instruction's write of that register, for which the compiler waits only in the other form.)
+template <typename T, bool THETA, bool STAGED>
 __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, TileOrder order) {
-  __shared__ u32x4 stage[3][PT * 64];
+  static_assert(!STAGED || sizeof(T) == 2, "an fp32 tile does not fit");
+  constexpr int STAGE = PT * 64;
+  __shared__ u32x4 lds[(STAGED ? 3 + PT - 1 : 3) * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KS = p.KS, panels_m = (p.M + 63) >> 6, panels_n = (p.N + 63) >> 6;
   // Workgroups are dealt to the eight XCDs in turn: each XCD takes a run of consecutive tiles, which go through the features for
   // eight tiles of tokens at a time, so that the tiles at work on an XCD share their operands in its L2.
   const uint32_t xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3;      // the grid is a multiple of 8
   const uint32_t first = xcd * (order.tiles >> 3) + min(xcd, order.tiles & 7), end = first + (order.tiles >> 3) + (xcd < (order.tiles & 7) ? 1 : 0);
-  auto locate = [&](Cursor& c) {
+  auto locate = [&](Cursor& c) __attribute__((always_inline)) {
     c.ok = c.t < end;
     const uint32_t t = c.ok ? c.t : first;
     c.l = order.layer.of(t);
@@ -397,9 +408,9 @@ __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, Tile
   locate(at);
   if (!at.ok) return;
   // (tiles and panels beyond the matrix: the last one again; what it gives is not stored)
-  auto panel_of = [&](const Cursor& c) { return Panel(p.b, (size_t)c.l * panels_n + min(c.panel, panels_n - 1), KS); };
+  auto panel_of = [&](const Cursor& c) __attribute__((always_inline)) { return Panel(p.b, (size_t)c.l * panels_n + min(c.panel, panels_n - 1), KS); };
   struct Tokens { Source codes, scales; uint32_t a1, s1; };
-  auto tokens_of = [&](const Cursor& c) {
+  auto tokens_of = [&](const Cursor& c) __attribute__((always_inline)) {
     const uint32_t second = c.tm * 2 + 1 < panels_m ? 1 : 0;      // the second panel of tokens
     return Tokens{Source(p.a.codes + (((size_t)c.l * panels_m * 4 + c.tm * PT) * KS << 10)),
                   Source(p.a.scales + (((size_t)c.l * panels_m + c.tm * 2) * KS << 8)), (second * 4 * KS) << 10, (second * KS) << 8};
@@ -411,11 +422,11 @@ __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, Tile
   u32x4 next[2], fa[4];
   PanelFrag fb[2];
   uint32_t sa[2][2];
-  auto load_a = [&]() {
+  auto load_a = [&]() __attribute__((always_inline)) {
     next[0] = A.codes.lanes16(lane, (uint32_t)(wave * KS + ca.ks) << 10);
     next[1] = A.codes.lanes16(lane, A.a1 + ((uint32_t)(wave * KS + ca.ks) << 10));
   };
-  auto advance_a = [&]() {
+  auto advance_a = [&]() __attribute__((always_inline)) {
     if (__builtin_expect(++ca.ks == KS, 0)) {
       ca.ks = 0;
       ca.t += per_xcd;
@@ -423,40 +434,85 @@ __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, Tile
       A = tokens_of(ca);
     }
   };
-  auto load_b = [&](int buf, int j) { fb[buf].c[j] = B.tile(j, cb.ks, lane); };
-  auto load_scales = [&](int buf) {
+  auto load_b = [&](int buf, int j) __attribute__((always_inline)) { fb[buf].c[j] = B.tile(j, cb.ks, lane); };
+  // STAGED: bias and threshold of the next tile, feature `lane` of the panel, fetched when cb comes to it
+  float bias_next = 0.f, theta_next = 0.f, theta_now = 0.f;
+  auto load_vectors = [&]() __attribute__((always_inline)) {
+    const size_t f = (size_t)cb.l * p.N + min(cb.panel * 64 + lane, p.N - 1);
+    if (p.bias) bias_next = p.bias[f];
+    if (THETA) theta_next = p.theta[f];
+  };
+  auto spread = [&](float v, int j, int k) __attribute__((always_inline)) { return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute((16 * j + 4 * (lane >> 4) + k) * 4, (int)__float_as_uint(v))); };
+  auto start = [&]() __attribute__((always_inline)) {
+    if constexpr (STAGED) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float b = spread(bias_next, j, k);
+#pragma unroll
+          for (int i = 0; i < PT; ++i) acc[i][j][k] = b;
+        }
+      theta_now = theta_next;
+    } else begin(p, at.l, at.panel, lane, acc);
+  };
+  auto load_scales = [&](int buf) __attribute__((always_inline)) {
     fb[buf].s = B.scale(cb.ks, lane);
     sa[buf][0] = S.scales.lanes4(lane, (uint32_t)cb.ks << 8);
     sa[buf][1] = S.scales.lanes4(lane, S.s1 + ((uint32_t)cb.ks << 8));
   };
-  auto advance_b = [&]() {
+  auto advance_b = [&]() __attribute__((always_inline)) {
     if (__builtin_expect(++cb.ks == KS, 0)) {
       cb.ks = 0;
       cb.t += per_xcd;
       locate(cb);
       B = panel_of(cb);
       S = tokens_of(cb);
+      if (STAGED) load_vectors();
     }
   };
-  auto put = [&](int st) {
+  auto put = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) stage[st][(wave + 4 * i) * 64 + lane] = next[i];
+    for (int i = 0; i < 2; ++i) lds[st * STAGE + (wave + 4 * i) * 64 + lane] = next[i];
   };
   load_a(); advance_a(); put(0);
   load_a(); advance_a(); put(1);
   load_a();
   for (int j = 0; j < 4; ++j) load_b(0, j);
   load_scales(0);
-  begin(p, at.l, at.panel, lane, acc);
+  if (STAGED) load_vectors();
+  start();
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fa[i] = stage[0][i * 64 + lane];
+  for (int i = 0; i < AHEAD; ++i) fa[i] = lds[i * 64 + lane];
   // One step: the features of the next step are fetched, the tokens of two steps on go to LDS (into the stage that the step before read)
   // and those of three steps on are fetched, one or two instructions of this at a time between the matrix instructions, which leave twelve
   // cycles each for others to issue.  Each tile's operand is read three tiles ahead, across the barrier as well: what is read before it
   // belongs to the next step and was written before the last barrier.
   int s0 = 0, s1 = 1, s2 = 2;
-  auto step = [&](auto i2) {
+  // STAGED, results under way: the next tile of 16 tokens to store, where it goes, and the bytes from there on that the buffer has
+  int out_next = PT, out_bytes = 0;
+  const int row_bytes = p.N * 2;
+  const char* out_at = static_cast<const char*>(p.out);
+  uint32_t out_lane = 0;      // offset of a lane's 16 bytes; beyond the buffer where its features are
+  const int out_lds = wave * 64 + ((lane & 56) | ((lane & 7) ^ (lane >> 3)));
+  u32x4 out[2];
+  auto out_read = [&]() __attribute__((always_inline)) {
+    const int at0 = (out_next == 0 ? s2 : 2 + min(out_next, PT - 1)) * STAGE + out_lds;
+    out[0] = lds[at0];
+    out[1] = lds[at0 + STAGE / 2];
+  };
+  auto out_store = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto d = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(out_at + h * 8 * (size_t)row_bytes), 0, max(out_bytes - h * 8 * row_bytes, 0), 0x00027000);
+      __builtin_amdgcn_raw_buffer_store_b128(out[h], d, (int)out_lane, 0, 2);      // (2: non-temporal)
+    }
+    ++out_next;
+    out_at += 16 * (size_t)row_bytes;
+    out_bytes = max(out_bytes - 16 * row_bytes, 0);
+  };
+  auto step = [&](auto i2) __attribute__((always_inline)) {
     constexpr int b = decltype(i2)::value;
     // (The branches of a step come before its matrix instructions: the compiler moved them into the block behind a branch, past the barrier.)
     advance_a();
@@ -469,7 +525,9 @@ __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, Tile
       if (i < 4) load_b(b ^ 1, i);
       if (i == PT - AHEAD - 1) put(s2);      // (at least AHEAD reads come behind it)
       if (i == 5) load_a();
-      fa[r & 3] = stage[r < PT ? s0 : s1][(r & (PT - 1)) * 64 + lane];
+      if (STAGED && i == 0) out_read();
+      if (STAGED && i == PT - 1) out_store();
+      fa[r & 3] = lds[(r < PT ? s0 : s1) * STAGE + (r & (PT - 1)) * 64 + lane];
       mfma4(i, fb[b], fa[i & 3], sa[b][i >> 2], acc[i]);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -483,14 +541,41 @@ __global__ __launch_bounds__(256, 2) void mx4_product_kernel(ProductArgs p, Tile
     const int s = s0;
     s0 = s1; s1 = s2; s2 = s;
     if (__builtin_expect(++at.ks < KS, 1)) return true;
-    finish<T, THETA>(p, at.l, at.tm * PT * 16, at.panel, lane, acc);
+    if constexpr (STAGED) {
+      while (out_next < PT) { out_read(); out_store(); }
+      f32x4 theta[4];
+      if (THETA) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) theta[j][k] = spread(theta_now, j, k);
+      }
+      const int t = lane & 7, q = lane >> 4, token0 = at.tm * PT * 16, f0 = at.panel * 64;
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int base = (i == 0 ? s2 : 2 + i) * STAGE + ((lane >> 3) & 1) * (STAGE / 2) + wave * 64 + t * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = !THETA || acc[i][j][k] > theta[j][k] ? acc[i][j][k] : 0.f;
+          reinterpret_cast<u32x2*>(lds + base + ((2 * j + (q >> 1)) ^ t))[q & 1] = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        }
+      }
+      out_next = 0;
+      out_at = static_cast<const char*>(p.out) + (((size_t)at.l * p.M + token0) * p.N + f0) * 2;
+      out_bytes = min(p.M - token0, PT * 16) * row_bytes;
+      out_lane = (lane & 7) * 8 < p.N - f0 ? (uint32_t)((lane >> 3) * row_bytes + (lane & 7) * 16) : 0x80000000u;
+    } else finish<T, THETA>(p, at.l, at.tm * PT * 16, at.panel, lane, acc);
     at.ks = 0;
     at.t += per_xcd;
     locate(at);
-    if (at.ok) begin(p, at.l, at.panel, lane, acc);
+    if (at.ok) start();
     return at.ok;
   };
   while (step(I<0>()) && step(I<1>())) {}
+  if (STAGED)
+    while (out_next < PT) { out_read(); out_store(); }
 }
 
 // Few tokens: bound by the bytes of B.  One workgroup takes one panel of 64 features by MT tiles of 16 tokens; its four wavefronts take
@@ -564,7 +649,17 @@ hipError_t launch_product(hipStream_t s, int L, const ProductArgs& p) {
   }
   const TileOrder order(L, tiles_m, tiles_n);
   const uint32_t grid = order.tiles >= WORKGROUPS ? WORKGROUPS : (order.tiles + 7) / 8 * 8;
-  hipLaunchKernelGGL((mx4_product_kernel<T, THETA>), dim3(grid), dim3(256), 0, s, p, order);
+  // Results through LDS where workgroups have four tiles and more, so that there is a next tile to store under, of up to 20 steps: beyond the
+  // eight that store something the others still read LDS in vain.  us staged / directly (L, M, N, K): 16, 4096, 8192, 128 201 / 224; the same, 512 239 / 258,
+  // 1024 363 / 384, 2048 610 / 617; 12, 4096, 6144, 768 176 / 195; the same, 2560 421 / 427; 16, 2048, 4096, 4096 295 / 289;
+  // 1, 16384, 2048, 256 (two tiles each) 20.2 / 19.3; 1, 4096, 2048, 768 (one) 11.7 / 9.7.
+  if constexpr (sizeof(T) == 2) {
+    if (order.tiles >= 4 * WORKGROUPS && p.KS <= 20) {
+      hipLaunchKernelGGL((mx4_product_kernel<T, THETA, true>), dim3(grid), dim3(256), 0, s, p, order);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((mx4_product_kernel<T, THETA, false>), dim3(grid), dim3(256), 0, s, p, order);
   return hipGetLastError();
 }
 
