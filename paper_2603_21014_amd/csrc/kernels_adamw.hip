@@ -11,8 +11,8 @@
 // Bound by memory: 10.03 bytes an element with bf16 weights and 8-bit moments, 22 with 32-bit ones.  The 8-bit form is not far from
 // the vector units' limit either (38 instructions an element; the two multiplications of the random
 // bits, the root and the reciprocal take four cycles each): with moments
-// unpacked and packed by shifts and selects (52) it was bound by them.  Measured: 738 M elements with 8-bit moments 1187 us, 6.2 TB/s
-// (1349 with 52 instructions and plain accesses); 425 M with 32-bit moments 1643 us, 5.7 TB/s (1754 with plain accesses).
+// unpacked and packed by shifts and selects (52) it was bound by them.  Measured: 738 M elements with 8-bit moments 1178 us, 6.3 TB/s
+// (1349 with 52 instructions and plain accesses); 425 M with 32-bit moments 1640 us, 5.7 TB/s (1754 with plain accesses).
 #include "../../include/clt.h"
 #include "common.h"
 
