@@ -256,7 +256,8 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  *
  * The functions of this part need no handle and no workspace of one; they allocate nothing, do not synchronise, may be
  * captured into a HIP graph, and report errors through clt_last_error(NULL).  Calls on different streams may overlap as
- * long as they do not share what they write. */
+ * long as they do not share what they write.  Outputs overlap neither inputs nor each other, except where a
+ * function says so; such calls are refused (clt_adamw_step: the list is the caller's to check). */
 
 /* Root-mean-square norm of residual streams, as a decoder-only language model applies it in front of an MLP: the
  * activations x[L,B,d] that a transcoder reads (Sec. 3.1 caches them).  Per row of d elements, all in fp32:
@@ -267,7 +268,7 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
  * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
  * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN gets codes 0 and a NaN as its scale.
- * Except for h, an output must not overlap an input.  1 <= L <= 128, B >= 1, L B < 2^30, d <= 2^20 a positive multiple of 8,
+ * 1 <= L <= 128, B >= 1, L B < 2^30, d <= 2^20 a positive multiple of 8,
  * eps > 0. */
 int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
                  const float* weight, float eps, void* h, void* y, int8_t* q, float* q_scale, float* rstd);

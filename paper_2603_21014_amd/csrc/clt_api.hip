@@ -8,6 +8,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <cmath>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -823,6 +825,26 @@ int clt_adam_step(clt_handle* h, void* stream, int64_t t, float lr, const clt_te
     }                                                                                          \
   } while (0)
 
+// What a call writes overlaps neither what it reads nor itself
+struct Span { const void* p; size_t bytes; };
+static bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x && y && x < y + b.bytes && y < x + a.bytes;
+}
+static bool apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span* w = written.begin(); w != written.end(); ++w) {
+    for (const Span* v = w + 1; v != written.end(); ++v)
+      if (overlap(*w, *v)) return false;
+    for (const Span& r : read)
+      if (overlap(*w, r)) return false;
+  }
+  return true;
+}
+#define APART(...)                                                                             \
+  do {                                                                                         \
+    if (!apart(__VA_ARGS__)) FAIL(CLT_ERR_INVALID_ARG, "%s: an output overlaps an input or another output", __func__); \
+  } while (0)
+
 static int check_rows(const char* who, int32_t L, int32_t B, int32_t d) {
   if (L < 1 || L > 128 || B < 1 || d < 8 || d > 1 << 20 || (d % 8) || (int64_t)L * B >= (int64_t)1 << 30)
     FAIL(CLT_ERR_SHAPE, "%s: unsupported shape L=%d B=%d d=%d (need 1<=L<=128, B>=1, L*B<2^30, d<=2^20 a positive multiple of 8)", who, L, B, d);
@@ -834,12 +856,14 @@ int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, c
   const int rc = check_rows(__func__, L, B, d);
   if (rc != CLT_OK) return rc;
   if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: bad dtype %d", dtype);
-  if (!(eps > 0.f)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: eps must be > 0");
+  if (!(eps > 0.f) || !std::isfinite(eps)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: eps must be > 0");
   NEED(x); NEED(weight);
   MAY(residual); MAY(h); MAY(y); MAY(q); MAY(q_scale); MAY(rstd);
   if ((residual != nullptr) != (h != nullptr)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: residual and h go together");
   if ((q != nullptr) != (q_scale != nullptr)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: q and q_scale go together");
   if (!y && !q) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: neither y nor q is given");
+  const size_t rows = (size_t)L * B, n = rows * d * (dtype == CLT_DTYPE_BF16 ? 2 : 4);
+  APART({{y, n}, {q, rows * d}, {q_scale, rows * 4}, {rstd, rows * 4}, {h == x || h == residual ? nullptr : h, n}}, {{x, n}, {residual, n}, {weight, (size_t)L * d * 4}});
   LAUNCH(launch_rms_norm(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, B, d,
                          RmsNormArgs{x, residual, weight, eps, h, y, q, q_scale, rstd}));
   return CLT_OK;
@@ -866,6 +890,9 @@ int clt_rms_norm_backward(void* stream, int32_t L, int32_t B, int32_t d, int32_t
     if (!workspace || misaligned(workspace) || workspace_bytes < need)
       FAIL(CLT_ERR_WORKSPACE, "clt_rms_norm_backward: workspace must be non-NULL, 16-byte aligned and at least %zu bytes (got %zu)", need, workspace_bytes);
   }
+  const size_t rows = (size_t)L * B, n = rows * d * (dtype == CLT_DTYPE_BF16 ? 2 : 4), w = (size_t)L * d * 4;
+  APART({{dx, n}, {dweight, w}, {dweight ? workspace : nullptr, workspace_bytes}},
+        {{h, n}, {weight, w}, {rstd, rows * 4}, {dy == dx ? nullptr : dy, n}, {dh == dx ? nullptr : dh, n}});
   LAUNCH(launch_rms_norm_backward(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, B, d,
                                   RmsNormBackwardArgs{h, weight, rstd, dy, dh, dx, dweight, static_cast<float*>(workspace)}));
   return CLT_OK;
@@ -875,13 +902,14 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
                    double beta2, double eps, uint64_t seed) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad list of tensors");
   if (t < 1) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: step count t must be >= 1");
-  if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 0x1p-126f))
+  if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 0x1p-126f) ||
+      !std::isfinite(lr) || !std::isfinite((float)eps))
     FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: need lr>=0, 0<=beta<1, eps>=2^-126");
   for (int32_t i = 0; i < n_tensors; ++i) {
     const clt_adamw_tensor& q = tensors[i];
     if (q.n < 0 || q.n > (int64_t)1 << 34) FAIL(CLT_ERR_SHAPE, "clt_adamw_step: tensor %d has n=%lld (need 0<=n<=2^34)", i, (long long)q.n);
     if ((q.dtype != CLT_DTYPE_F32 && q.dtype != CLT_DTYPE_BF16) || (q.grad_dtype != CLT_DTYPE_F32 && q.grad_dtype != CLT_DTYPE_BF16) ||
-        (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f))
+        (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f) || !std::isfinite(q.weight_decay))
       FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: bad dtype, grad_dtype, state_bits or weight_decay", i);
     if (q.n == 0) continue;
     if (!q.p || !q.g || !q.m || !q.v) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: p, g, m and v are required", i);
@@ -943,6 +971,8 @@ int clt_mx4_quantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t d
   NEED(a); NEED(codes); NEED(scales);
   if (int8) NEED(a_scale);
   else if (a_scale) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_quantise: a_scale given but input_format is native");
+  const size_t n = (size_t)L * rows * K, tiles = (size_t)L * mx4_panels(rows) * mx4_steps(K);
+  APART({{codes, tiles * 4096}, {scales, tiles * 256}}, {{a, n * (int8 ? 1 : dtype == CLT_DTYPE_BF16 ? 2 : 4)}, {a_scale, (size_t)L * rows * 4}});
   LAUNCH(launch_mx4_quantise(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, int8, transposed != 0, L, rows, K, a, a_scale,
                              static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales)));
   return CLT_OK;
@@ -954,6 +984,8 @@ int clt_mx4_dequantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t
   if (rc != CLT_OK) return rc;
   if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_dequantise: bad dtype %d", dtype);
   NEED(codes); NEED(scales); NEED(out);
+  const size_t tiles = (size_t)L * mx4_panels(rows) * mx4_steps(K);
+  APART({{out, (size_t)L * rows * K * (dtype == CLT_DTYPE_BF16 ? 2 : 4)}}, {{codes, tiles * 4096}, {scales, tiles * 256}});
   LAUNCH(launch_mx4_dequantise(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, rows, K,
                                Mx4{static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales)}, out));
   return CLT_OK;
@@ -969,6 +1001,8 @@ int clt_mx4_product(void* stream, int32_t L, int32_t M, int32_t N, int32_t K, co
   if (dtype != CLT_DTYPE_F32 && dtype != CLT_DTYPE_BF16) FAIL(CLT_ERR_INVALID_ARG, "clt_mx4_product: bad dtype %d", dtype);
   NEED(a_codes); NEED(a_scales); NEED(b_codes); NEED(b_scales); NEED(out);
   MAY(bias); MAY(theta);
+  const size_t ta = (size_t)L * mx4_panels(M) * mx4_steps(K), tb = (size_t)L * mx4_panels(N) * mx4_steps(K), v = (size_t)L * N * 4;
+  APART({{out, (size_t)L * M * N * (dtype == CLT_DTYPE_BF16 ? 2 : 4)}}, {{a_codes, ta * 4096}, {a_scales, ta * 256}, {b_codes, tb * 4096}, {b_scales, tb * 256}, {bias, v}, {theta, v}});
   LAUNCH(launch_mx4_product(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, M, N, K,
                             Mx4{static_cast<const uint8_t*>(a_codes), static_cast<const uint8_t*>(a_scales)},
                             Mx4{static_cast<const uint8_t*>(b_codes), static_cast<const uint8_t*>(b_scales)}, bias, theta, out));

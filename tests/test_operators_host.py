@@ -35,7 +35,7 @@ def test_rms_norm_refusals(K):
     for bad in (dict(L=0), dict(L=129), dict(B=0), dict(B=-1), dict(d=0), dict(d=12), dict(d=(1 << 20) + 8), dict(L=128, B=1 << 24)):
         refused(K, -2, "shape", call(**bad))
     refused(K, -1, "dtype", call(dtype=2))
-    for eps in (0.0, -1.0, float("nan")):
+    for eps in (0.0, -1.0, float("nan"), float("inf")):
         refused(K, -1, "eps", call(eps=eps))
     refused(K, -1, "argument x is NULL", call(x=None))
     refused(K, -1, "weight is NULL", call(weight=None))
@@ -83,11 +83,11 @@ def test_adamw_refusals(K):
     refused(K, -1, "list", call(count=-1))
     assert K._lib.clt_adamw_step(None, 1, None, 1, 1e-3, 0.9, 0.999, 1e-8, 0) == -1
     refused(K, -1, "step count", call(tensor(), t=0))
-    for bad in (dict(lr=-1.0), dict(lr=float("nan")), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39)):
+    for bad in (dict(lr=-1.0), dict(lr=float("nan")), dict(lr=float("inf")), dict(eps=float("inf")), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39)):
         refused(K, -1, "scalar", call(tensor(), **bad))
     refused(K, -2, "tensor 1", call(tensor(**good8), tensor(n=-1)))
     refused(K, -2, "tensor 0", call(tensor(n=(1 << 34) + 1)))
-    for bad in (dict(dtype=2), dict(grad_dtype=2), dict(bits=16), dict(decay=-0.1), dict(decay=float("nan"))):
+    for bad in (dict(dtype=2), dict(grad_dtype=2), dict(bits=16), dict(decay=-0.1), dict(decay=float("nan")), dict(decay=float("inf"))):
         refused(K, -1, "tensor 1", call(tensor(), tensor(**bad)))
     for name in ("p", "g", "m", "v"):
         refused(K, -1, "required", call(tensor(**{name: None})))
@@ -99,6 +99,36 @@ def test_adamw_refusals(K):
     refused(K, -3, "aligned", call(tensor(master=ODD)))
     # nothing to do is no error, and needs no device
     assert call(count=0) == 0 and call(tensor(n=0, p=None, g=None, m=None, v=None)) == 0
+
+
+def test_outputs_that_overlap_are_refused(K):
+    at = lambda k: (k + 1) << 24      # places 16 MB apart
+    L, B, d = 2, 3, 64
+    n = L * B * d * 2
+
+    def norm(**kw):
+        a = dict(x=at(0), residual=at(1), weight=at(2), h=at(3), y=at(4), q=at(5), q_scale=at(6), rstd=at(7))
+        a.update(kw)
+        return K._lib.clt_rms_norm(None, L, B, d, K.DTYPE_BF16, a["x"], a["residual"], a["weight"], 1e-5, a["h"], a["y"], a["q"], a["q_scale"], a["rstd"])
+    for kw in (dict(y=at(0)), dict(y=at(1) + n - 16), dict(y=at(3)), dict(q=at(0) + 16), dict(q=at(4)), dict(q_scale=at(2)), dict(rstd=at(6)), dict(h=at(0) + 16), dict(h=at(1) - 16),
+               dict(h=at(2)), dict(h=at(0), y=at(0))):
+        refused(K, -1, "overlaps", norm(**kw))
+
+    def back(**kw):
+        a = dict(h=at(0), weight=at(1), rstd=at(2), dy=at(3), dh=at(4), dx=at(5), dweight=at(6), ws=at(7))
+        a.update(kw)
+        return K._lib.clt_rms_norm_backward(None, L, B, d, K.DTYPE_BF16, a["h"], a["weight"], a["rstd"], a["dy"], a["dh"], a["dx"], a["dweight"], a["ws"], 1 << 20)
+    for kw in (dict(dx=at(0)), dict(dx=at(3) + 16), dict(dx=at(4) - 16), dict(dweight=at(1)), dict(dweight=at(5)), dict(ws=at(0)), dict(ws=at(6) - 16), dict(dx=at(2))):
+        refused(K, -1, "overlaps", back(**kw))
+    rows, Kd = 24, 64
+    for a, s, c, sc in ((at(0), None, at(0), at(2)), (at(0), None, at(1), at(1) + 4096), (at(0), None, at(1), at(0) + 16)):
+        refused(K, -1, "overlaps", K._lib.clt_mx4_quantise(None, L, rows, Kd, K.DTYPE_BF16, K.INPUT_NATIVE, 0, a, s, c, sc))
+    refused(K, -1, "overlaps", K._lib.clt_mx4_quantise(None, L, rows, Kd, K.DTYPE_BF16, K.INPUT_INT8_ROWSCALE, 0, at(0), at(1), at(2), at(1)))
+    for c, s, o in ((at(0), at(1), at(0) + 4096), (at(0), at(1), at(1))):
+        refused(K, -1, "overlaps", K._lib.clt_mx4_dequantise(None, L, rows, Kd, 1, c, s, o))
+    for k in range(6):
+        args = [at(i) for i in range(6)]
+        refused(K, -1, "overlaps", K._lib.clt_mx4_product(None, L, 5, 24, Kd, *args, 0, args[k] + 16))
 
 
 def test_mx4_refusals(K):
