@@ -354,11 +354,12 @@ __device__ __forceinline__ void finish(const ProductArgs& p, int l, int token0, 
 // features by all the tokens (8 x 4 accumulators of 16 x 16).  A panel is read by one wavefront only and goes from memory into its
 // registers, one step ahead; the tokens are fetched three steps ahead and staged in LDS, in three stages of one step each.  Both run on
 // into the next tile.  Two workgroups share a compute unit, so that one's epilogue runs under the other's matrix instructions.
-// Measured: 16 layers of 4096 by 8192 by K = 2048 610 us, 3.6 PFLOP/s (bare loop of the instruction on random operands 7.2, with the LDS reads and the barrier 6.5).  What bounds
-// it: the way of the operands into the registers.  32 matrix instructions of 16 cycles take 4 KB of features through the vector cache and 8 KB of
-// tokens out of LDS, and with two wavefronts on a SIMD both ways are busy three quarters of a step that has no pause (on zeros, where power is no limit, the loop
-// reaches 5.4 PFLOP/s of 9.7); on random numbers the clock falls to 1.96 GHz as well.  A tile of 128 by 128 to a wavefront would need
-// a third fewer operands and all registers of a SIMD, with no second workgroup for the epilogue to hide under.
+// Measured: 16 layers of 4096 by 8192 by K = 2048 610 us, 3.6 PFLOP/s (bare loop of the instruction on random operands 7.2, with the LDS reads and the barrier
+// 6.5); at K = 32768 4.5 on random numbers and 5.3 on zeros, where power is no limit.  What bounds it besides power: the operands' way through the vector cache,
+// 64 bytes a cycle.  A wavefront's step takes 6.75 KB that way, which is 860 cycles for the eight of a compute unit, beside 1024 of matrix instructions (the
+// LDS, 256 bytes a cycle, is busy 40 %).  The same shape with half of the features' loads left out 600 us in a run where it took 632, without them 566, without the
+// tokens' as well 533.  A tile of 128 by 128 to a wavefront would need a third fewer operands and all registers of a SIMD, with no second
+// workgroup for the epilogue to hide under.
 constexpr int PT = 8;             // tiles of 16 tokens
 constexpr int AHEAD = 3;          // of these, the operands under way from LDS
 constexpr int WORKGROUPS = 512;   // two on each of 256 compute units
