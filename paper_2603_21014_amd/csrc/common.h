@@ -48,6 +48,17 @@ __device__ __forceinline__ void nt_store_f4(float* p, float4 v) {
   CLT_NT_STORE(t, reinterpret_cast<nt_f32x4*>(p));
 }
 
+// 16, 8 or 4 bytes; STREAM: past the caches, for calls that touch more than the Infinity Cache holds
+template <bool STREAM, typename V> __device__ __forceinline__ V take(const void* p) {
+  const V* q = static_cast<const V*>(p);
+  return STREAM ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool STREAM, typename V> __device__ __forceinline__ void give(void* p, V v) {
+  V* q = static_cast<V*>(p);
+  if (STREAM) __builtin_nontemporal_store(v, q);
+  else *q = v;
+}
+
 // Element-type traits for the two storage types.
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -122,6 +133,9 @@ __device__ __forceinline__ void adam_element(float& p, float& m, float& v, float
 template <int CTRL> __device__ __forceinline__ float dpp_move(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
 }
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_move(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
 __device__ __forceinline__ float row16_sum(float v) {
   v += dpp_move<0xB1>(v);    // quad_perm [1,0,3,2]
   v += dpp_move<0x4E>(v);    // quad_perm [2,3,0,1]
@@ -129,6 +143,9 @@ __device__ __forceinline__ float row16_sum(float v) {
   v += dpp_move<0x140>(v);   // row_mirror: the other half row
   return v;
 }
+
+// Scale of an 8- or 4-bit block: 2^(s-127), NaN for s = 255
+__device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? 0x1p-127f : __uint_as_float(s << 23); }
 
 // act_class bits
 constexpr uint8_t CLS_ACTIVE = 1;

@@ -32,9 +32,6 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_move(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
-}
 __device__ __forceinline__ uint32_t row16_max(uint32_t v) {      // as row16_sum
   v = max(v, dpp_move<0xB1>(v));
   v = max(v, dpp_move<0x4E>(v));
@@ -61,8 +58,6 @@ template <int MANT, int BIAS, int TOP> struct Float8 {
 };
 typedef Float8<3, 7, 8> E4M3;
 typedef Float8<2, 15, 15> E5M2;
-// 2^(s-127), NaN for s = 255
-__device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? 0x1p-127f : __uint_as_float(s << 23); }
 // the top bytes of four words
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0703u), hi = __builtin_amdgcn_perm(d, c, 0x07030c0cu);
@@ -76,17 +71,6 @@ __device__ __forceinline__ void decode_m(uint32_t c, float f, float* x) {
 __device__ __forceinline__ void decode_v(uint32_t c, float f, float* x) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_bf8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_bf8((int)c, true);
   x[0] = a[0] * f; x[1] = a[1] * f; x[2] = b[0] * f; x[3] = b[1] * f;
-}
-
-// 16 or 8 bytes, STREAM: past the caches (see launch_adamw)
-template <bool STREAM, typename V> __device__ __forceinline__ V take(const void* p) {
-  const V* q = static_cast<const V*>(p);
-  return STREAM ? __builtin_nontemporal_load(q) : *q;
-}
-template <bool STREAM, typename V> __device__ __forceinline__ void give(void* p, V v) {
-  V* q = static_cast<V*>(p);
-  if (STREAM) __builtin_nontemporal_store(v, q);
-  else *q = v;
 }
 
 // Eight elements of a lane from or to memory.  ROW: consecutive ones (a block of 8-bit moments is sixteen such lanes); else two runs of four

@@ -41,9 +41,6 @@ __device__ __forceinline__ uint32_t to_codes(const float* x, uint32_t s) {
   return s == 255u ? 0u : w;
 }
 
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_move(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
-}
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   v = max(v, dpp_move<0xB1>(v));          // quad_perm [1,0,3,2]
   return max(v, dpp_move<0x4E>(v));       // quad_perm [2,3,0,1]
@@ -170,9 +167,6 @@ __global__ __launch_bounds__(256) void mx4_quantise_transposed_kernel(int rows, 
     scales[((size_t)l * panels * KS << 8) + scale_offset(r + c, kb, KS)] = (uint8_t)e;
   }
 }
-
-// 2^(s-127), NaN for s = 255
-__device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? 0x1p-127f : __uint_as_float(s << 23); }
 
 // The way back, cut as the way there: a wavefront takes 16 rows by one step; the lanes of a quad exchange the words of their four blocks, so that each
 // has eight consecutive elements of each block.  12 layers of 6144 rows of 768 into bf16 (143 MB): 22.8 us, 6.3 TB/s.

@@ -37,17 +37,6 @@ __device__ __forceinline__ u32x4 narrow16(const float (&f)[4]) {
   return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
 }
 
-// 16, 8 or 4 bytes, STREAM: past the caches (see streams())
-template <bool STREAM, typename V> __device__ __forceinline__ V take(const void* p) {
-  const V* q = static_cast<const V*>(p);
-  return STREAM ? __builtin_nontemporal_load(q) : *q;
-}
-template <bool STREAM, typename V> __device__ __forceinline__ void give(void* p, V v) {
-  V* q = static_cast<V*>(p);
-  if (STREAM) __builtin_nontemporal_store(v, q);
-  else *q = v;
-}
-
 // What the codes and the scale of a row follow from
 struct RowScale { float rstd, k, scale; bool broken; };
 __device__ __forceinline__ RowScale row_scale(float sum, uint32_t top, float eps, int d) {
