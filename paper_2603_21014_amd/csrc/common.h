@@ -32,8 +32,8 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f) { return (bf16_t)(pack_bf
 
 // Streaming (non-temporal) 16- and 8-byte accesses for the optimizer state and weights in the
 // update epilogues of the contractions: data touched once there should not displace the operand
-// panels that the contractions reuse out of the L2.  (Kernels that do nothing but stream are
-// faster with plain accesses and do not use these.)
+// panels that the contractions reuse out of the L2.  (Kernels that do nothing but stream over less than the
+// Infinity Cache holds are faster with plain accesses and do not use these.)
 typedef float nt_f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int nt_u32x2 __attribute__((ext_vector_type(2)));
 #define CLT_NT_LOAD(p) __builtin_nontemporal_load(p)
