@@ -107,9 +107,9 @@ def _check(rc, handle=None):
         raise CLTError(rc, _lib.clt_last_error(handle).decode())
 
 
-def _stream():
+def _stream(device=None):
     # (by its pointer: making a torch.cuda.Stream object of it takes 2.7 us of a call's 9)
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 def _ptr(t, shape, dtype, name, optional=False):
@@ -339,7 +339,7 @@ def clt_rms_norm(x, weight, eps, y=None, q=None, q_scale=None, residual=None, h=
     dt, T, s, f32 = _storage(x, "x"), x.dtype, x.shape, torch.float32
     L, B, d = s
     _check(_lib.clt_rms_norm(
-        _stream(), L, B, d, dt, _arg(x, dev, s, T, "x"), _may(residual, dev, s, T, "residual"), _arg(weight, dev, (L, d), f32, "weight"), eps,
+        _stream(dev), L, B, d, dt, _arg(x, dev, s, T, "x"), _may(residual, dev, s, T, "residual"), _arg(weight, dev, (L, d), f32, "weight"), eps,
         _may(h, dev, s, T, "h"), _may(y, dev, s, T, "y"), _may(q, dev, s, torch.int8, "q"), _may(q_scale, dev, (L, B), f32, "q_scale"),
         _may(rstd, dev, (L, B), f32, "rstd")))
 
@@ -365,7 +365,7 @@ def clt_rms_norm_backward(h, weight, rstd, dy, dx, dweight=None, workspace=None,
     dt, T, s, f32 = _storage(h, "h"), h.dtype, h.shape, torch.float32
     L, B, d = s
     _check(_lib.clt_rms_norm_backward(
-        _stream(), L, B, d, dt, _arg(h, dev, s, T, "h"), _arg(weight, dev, (L, d), f32, "weight"), _arg(rstd, dev, (L, B), f32, "rstd"),
+        _stream(dev), L, B, d, dt, _arg(h, dev, s, T, "h"), _arg(weight, dev, (L, d), f32, "weight"), _arg(rstd, dev, (L, B), f32, "rstd"),
         _arg(dy, dev, s, T, "dy"), _may(dh, dev, s, T, "dh"), _arg(dx, dev, s, T, "dx"), _may(dweight, dev, (L, d), f32, "dweight"),
         *_room(workspace, dev)))
 
@@ -441,7 +441,7 @@ class AdamW:
     def step(self, t, lr):
         if self.device is not None and torch.cuda.current_device() != self.device:
             raise ValueError(f"the tensors are on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
-        _check(_lib.clt_adamw_step(_stream(), len(self.tensors), self._array, t, lr, *self.scalars))
+        _check(_lib.clt_adamw_step(_stream(self.device), len(self.tensors), self._array, t, lr, *self.scalars))
 
 
 def clt_mx4_bytes(L, rows, K):
@@ -479,7 +479,7 @@ def clt_mx4_quantise(a, codes, scales, a_scale=None, transposed=False):
         dt, fmt = _storage(a, "a"), INPUT_NATIVE
     s = a.shape
     L, rows, K = (s[0], s[2], s[1]) if transposed else s
-    _check(_lib.clt_mx4_quantise(_stream(), L, rows, K, dt, fmt, int(transposed), _arg(a, dev, s, a.dtype, "a"),
+    _check(_lib.clt_mx4_quantise(_stream(dev), L, rows, K, dt, fmt, int(transposed), _arg(a, dev, s, a.dtype, "a"),
                                  _may(a_scale, dev, (L, rows), torch.float32, "a_scale"), *_packed(codes, scales, dev, L, rows, K, "")))
 
 
@@ -488,7 +488,7 @@ def clt_mx4_dequantise(codes, scales, out):
     dev = _device_of(out, "out")
     dt, s = _storage(out, "out"), out.shape
     L, rows, K = s
-    _check(_lib.clt_mx4_dequantise(_stream(), L, rows, K, dt, *_packed(codes, scales, dev, L, rows, K, ""), _arg(out, dev, s, out.dtype, "out")))
+    _check(_lib.clt_mx4_dequantise(_stream(dev), L, rows, K, dt, *_packed(codes, scales, dev, L, rows, K, ""), _arg(out, dev, s, out.dtype, "out")))
 
 
 def clt_mx4_product(a_codes, a_scales, b_codes, b_scales, out, K, bias=None, theta=None):
@@ -496,7 +496,7 @@ def clt_mx4_product(a_codes, a_scales, b_codes, b_scales, out, K, bias=None, the
     dev = _device_of(out, "out")
     dt, s, f32 = _storage(out, "out"), out.shape, torch.float32
     L, M, N = s
-    _check(_lib.clt_mx4_product(_stream(), L, M, N, K, *_packed(a_codes, a_scales, dev, L, M, K, "a_"), *_packed(b_codes, b_scales, dev, L, N, K, "b_"),
+    _check(_lib.clt_mx4_product(_stream(dev), L, M, N, K, *_packed(a_codes, a_scales, dev, L, M, K, "a_"), *_packed(b_codes, b_scales, dev, L, N, K, "b_"),
                                 _may(bias, dev, (L, N), f32, "bias"), _may(theta, dev, (L, N), f32, "theta"), dt, _arg(out, dev, s, out.dtype, "out")))
 
 
