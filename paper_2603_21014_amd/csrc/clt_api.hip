@@ -863,7 +863,7 @@ int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, c
   if ((q != nullptr) != (q_scale != nullptr)) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: q and q_scale go together");
   if (!y && !q) FAIL(CLT_ERR_INVALID_ARG, "clt_rms_norm: neither y nor q is given");
   const size_t rows = (size_t)L * B, n = rows * d * (dtype == CLT_DTYPE_BF16 ? 2 : 4);
-  APART({{y, n}, {q, rows * d}, {q_scale, rows * 4}, {rstd, rows * 4}, {h == x || h == residual ? nullptr : h, n}}, {{x, n}, {residual, n}, {weight, (size_t)L * d * 4}});
+  APART({{y, n}, {q, rows * d}, {q_scale, rows * 4}, {rstd, rows * 4}, {h, n}}, {{h == x ? nullptr : x, n}, {h == residual ? nullptr : residual, n}, {weight, (size_t)L * d * 4}});
   LAUNCH(launch_rms_norm(static_cast<hipStream_t>(stream), dtype == CLT_DTYPE_BF16, L, B, d,
                          RmsNormArgs{x, residual, weight, eps, h, y, q, q_scale, rstd}));
   return CLT_OK;

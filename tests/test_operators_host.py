@@ -131,6 +131,25 @@ def test_outputs_that_overlap_are_refused(K):
         refused(K, -1, "overlaps", K._lib.clt_mx4_product(None, L, 5, 24, Kd, *args, 0, args[k] + 16))
 
 
+def test_norm_in_place_keeps_its_other_inputs_apart(K):
+    """The sum may overwrite x or residual, but not a part of the other one or the weights under it."""
+    at = lambda k: (k + 1) << 24
+    n = 2 * 3 * 64 * 2
+
+    def norm(x, residual, weight, h):
+        return K._lib.clt_rms_norm(None, 2, 3, 64, K.DTYPE_BF16, x, residual, weight, 1e-5, h, at(7), None, None, None)
+    for a, b in ((at(0), at(0) + 128), (at(0), at(0) - 128), (at(0), at(0) + n - 16), (at(0) + 16, at(0))):
+        refused(K, -1, "overlaps", norm(a, b, at(2), a))
+        refused(K, -1, "overlaps", norm(a, b, at(2), b))
+    for w in (at(0), at(0) + n - 16, at(0) - 2 * 64 * 4 + 16):
+        refused(K, -1, "overlaps", norm(at(0), at(1), w, at(0)))
+        refused(K, -1, "overlaps", norm(at(1), at(0), w, at(0)))
+    # one buffer as both operands holds twice itself afterwards, and neighbours are no overlap: these get as far as the device
+    for args in ((at(0), at(0), at(2), at(0)), (at(0), at(0) + n, at(2), at(0)), (at(0), at(1), at(0) + n, at(0))):
+        if not torch.cuda.is_available():
+            assert norm(*args) == -5, K._lib.clt_last_error(None)
+
+
 def test_mx4_refusals(K):
     assert K.clt_mx4_bytes(3, 65, 136) == (3 * 2 * 2 * 4096, 3 * 2 * 2 * 256)
     for bad in ((0, 8, 64), (1, 0, 64), (1, 8, 0), (1, 8, 12), (65536, 8, 64), (1, (1 << 20) + 1, 64), (1, 1 << 20, 1 << 16), (1, 8, (1 << 22) + 8)):
