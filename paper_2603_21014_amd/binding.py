@@ -605,12 +605,16 @@ class CLTStep:
 
     def adamw(self, params, bits=8, master=None, weight_decay=0.0, seed=0):
         """An AdamW over this step's gradients for train_step: moments of the matrices in 8 or 32 bits, beginning at zero, those
-        of the vectors in 32; weight decay and master copies for the matrices.  Needs matrix_grads."""
+        of the vectors in 32; weight decay and master copies for the matrices.  Needs matrix_grads, and with master_weights a
+        master of both matrices."""
         if "W_dec" not in self.grads:
             raise ValueError("adamw needs the matrices' gradients (matrix_grads=True)")
+        matrices = ("W_enc", "W_dec")
+        if self.cfg.master_weights and any((master or {}).get(k) is None for k in matrices):
+            raise ValueError("master_weights: adamw needs the master copies of W_enc and W_dec")
         tensors = []
         for k, g in self.grads.items():
-            matrix = k in ("W_enc", "W_dec")
+            matrix = k in matrices
             tensors.append(AdamWTensor(params[k], g, *AdamW.moments(params[k], bits if matrix else 32), (master or {}).get(k) if matrix else None,
                                        weight_decay if matrix else 0.0))
         return AdamW(tensors, *self.adam, seed)

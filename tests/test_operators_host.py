@@ -312,3 +312,40 @@ def test_oracle_mx4_packing_and_rounding():
     bad = np.zeros((1, 2, 32), np.float32)
     bad[0, 0, 5], bad[0, 1, 6] = np.nan, -np.inf
     assert R.mx4_round(bad)[1][0, :, 0].tolist() == [255, 255]
+
+
+# ---- the optimiser inside the training step: what it may be given -------------------------------------------------------
+
+class _Step:
+    """A CLTStep without a device: tensors on the host, and its GPU calls written down instead of made."""
+
+    def __new__(cls, K, **config):
+        step = object.__new__(K.CLTStep)
+        L, d, F, B = 2, 64, 136, 8
+        step.cfg = K.make_config(L, d, F, B, K.DTYPE_BF16, **config)
+        step.adam = (0.9, 0.999, 1e-8)
+        f32, T = torch.float32, torch.bfloat16
+        step.grads = {"b_enc": torch.zeros(L, F), "theta": torch.zeros(L, F), "b_dec": torch.zeros(L, d), "W_enc": torch.zeros(L, d, F, dtype=T),
+                      "W_dec": torch.zeros(3, F, d, dtype=T)}
+        step.calls = []
+        for name in ("forward", "loss", "backward", "backward_adam_step", "adam_step"):
+            setattr(step, name, lambda *a, name=name, **k: step.calls.append(name))
+        return step
+
+
+def test_adamw_of_a_step_with_master_weights_needs_them(K, monkeypatch):
+    made = []
+    monkeypatch.setattr(K, "AdamWTensor", lambda *a: made.append(a))
+    monkeypatch.setattr(K, "AdamW", type("List", (), {"__init__": lambda self, *a: None, "moments": K.AdamW.moments}))
+    step = _Step(K, master_weights=True)
+    params = {k: g.clone() for k, g in step.grads.items()}
+    master = {k: params[k].float() for k in ("W_enc", "W_dec")}
+    for bad in (None, {}, {"W_enc": master["W_enc"]}, {"W_dec": master["W_dec"]}, dict(master, W_enc=None)):
+        with pytest.raises(ValueError, match="master"):
+            step.adamw(params, master=bad)
+    assert not made
+    step.adamw(params, master=master)
+    assert [a[6] is not None for a in made] == [False, False, False, True, True]
+    made.clear()      # without the flag they may be left out
+    _Step(K).adamw(params)
+    assert [a[6] for a in made] == [None] * 5
