@@ -619,10 +619,21 @@ class CLTStep:
                                        weight_decay if matrix else 0.0))
         return AdamW(tensors, *self.adam, seed)
 
+    def _check_optimiser(self, optimiser, params):
+        """What an AdamW updates from this step's gradients has to be the parameters that the step reads."""
+        mine = {g.data_ptr(): params[k].data_ptr() for k, g in self.grads.items()}
+        held = [(t.c.g, t.c.p) for t in optimiser.tensors if t.c.g in mine]
+        if not held:
+            raise ValueError("the optimiser holds none of this step's gradients")
+        if any(mine[g] != p for g, p in held):
+            raise ValueError("the optimiser holds other parameters than the step is given")
+
     def train_step(self, x, y, params, m, v, t, lr, lambda0, master=None, x_scale=None, y_scale=None, fused=True,
                    lambda1=0.0, optimiser=None):
         """forward, loss, backward and Adam; `fused` runs Adam inside the weight-gradient GEMMs.  With an optimiser (see adamw) its
-        step takes Adam's place: m, v, master and fused are not used."""
+        step takes Adam's place: m, v, master and fused are not used, and what it updates from this step's gradients has to be params."""
+        if isinstance(optimiser, AdamW):
+            self._check_optimiser(optimiser, params)
         self.forward(x, params, x_scale)
         self.loss(y, lambda0, y_scale, False, lambda1, params)
         if optimiser is not None:

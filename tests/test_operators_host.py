@@ -2,6 +2,7 @@
 oracle that the GPU tests compare with (gradients against differences, formats against torch's, rounding without bias)."""
 import ctypes
 import os
+import types
 
 import numpy as np
 import pytest
@@ -349,3 +350,39 @@ def test_adamw_of_a_step_with_master_weights_needs_them(K, monkeypatch):
     made.clear()      # without the flag they may be left out
     _Step(K).adamw(params)
     assert [a[6] for a in made] == [None] * 5
+
+
+def test_train_step_takes_an_optimiser_of_its_own_parameters_only(K):
+    step = _Step(K)
+    params = {k: g.clone() for k, g in step.grads.items()}
+
+    def optimiser(p, g):
+        """An AdamW over p and g; steps are written down."""
+        opt = object.__new__(K.AdamW)
+        opt.tensors = [types.SimpleNamespace(c=K.clt_adamw_tensor(p=p[k].data_ptr(), g=g[k].data_ptr())) for k in p]
+        opt.step = lambda t, lr: step.calls.append("adamw")
+        return opt
+
+    def train(opt):
+        step.calls.clear()
+        step.train_step(None, None, params, None, None, 1, 1e-3, 1.0, optimiser=opt)
+    other = {k: p.clone() for k, p in params.items()}
+    for bad in (optimiser(other, step.grads),                                       # the forward pass would read what no step writes
+                optimiser(dict(params, W_dec=other["W_dec"]), step.grads),
+                optimiser(params, {k: g.clone() for k, g in step.grads.items()}),   # gradients of another step
+                optimiser({}, {})):
+        with pytest.raises(ValueError, match="optimiser"):
+            train(bad)
+        assert not step.calls
+    train(optimiser(params, step.grads))
+    assert step.calls == ["forward", "loss", "backward", "adamw"]
+    # a part of the parameters, or others beside them, are the caller's choice
+    train(optimiser({"W_enc": params["W_enc"]}, step.grads))
+    train(optimiser(dict(params, more=other["W_enc"]), dict(step.grads, more=other["W_dec"])))
+    old = optimiser(params, step.grads)
+    params["W_enc"] = params["W_enc"].clone()      # other memory than the list was made for
+    with pytest.raises(ValueError, match="optimiser"):
+        train(old)
+    step.calls.clear()
+    step.train_step(None, None, params, None, None, 1, 1e-3, 1.0, fused=False)
+    assert step.calls == ["forward", "loss", "backward", "adam_step"]
