@@ -905,11 +905,13 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
   if (!(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 0x1p-126f) ||
       !std::isfinite(lr) || !std::isfinite((float)eps))
     FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: need lr>=0, 0<=beta<1, eps>=2^-126");
+  const double bc1 = 1.0 - pow(beta1, (double)t), bc2 = 1.0 - pow(beta2, (double)t);
+  if (!std::isfinite((float)(lr / bc1))) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: bad scalar: lr / (1 - beta1^t) is no finite float");
   for (int32_t i = 0; i < n_tensors; ++i) {
     const clt_adamw_tensor& q = tensors[i];
     if (q.n < 0 || q.n > (int64_t)1 << 34) FAIL(CLT_ERR_SHAPE, "clt_adamw_step: tensor %d has n=%lld (need 0<=n<=2^34)", i, (long long)q.n);
     if ((q.dtype != CLT_DTYPE_F32 && q.dtype != CLT_DTYPE_BF16) || (q.grad_dtype != CLT_DTYPE_F32 && q.grad_dtype != CLT_DTYPE_BF16) ||
-        (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f) || !std::isfinite(q.weight_decay))
+        (q.state_bits != 8 && q.state_bits != 32) || !(q.weight_decay >= 0.f) || !std::isfinite((float)(lr * (double)q.weight_decay)))
       FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: bad dtype, grad_dtype, state_bits or weight_decay", i);
     if (q.n == 0) continue;
     if (!q.p || !q.g || !q.m || !q.v) FAIL(CLT_ERR_INVALID_ARG, "clt_adamw_step: tensor %d: p, g, m and v are required", i);
@@ -918,7 +920,6 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
     if (misaligned(q.p) || misaligned(q.g) || misaligned(q.m) || misaligned(q.v) || misaligned(q.m_scale) || misaligned(q.v_scale) || misaligned(q.master))
       FAIL(CLT_ERR_ALIGN, "clt_adamw_step: tensor %d: a pointer is not 16-byte aligned", i);
   }
-  const double bc1 = 1.0 - pow(beta1, (double)t), bc2 = 1.0 - pow(beta2, (double)t);
   AdamWList list{};
   list.a = AdamScalars{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 / bc2), (float)(-lr / bc1), (float)eps};
   const uint32_t key_t = adamw_mix((uint32_t)((uint64_t)t >> 32)) ^ (uint32_t)t;

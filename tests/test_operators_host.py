@@ -102,6 +102,18 @@ def test_adamw_refusals(K):
     assert call(count=0) == 0 and call(tensor(n=0, p=None, g=None, m=None, v=None)) == 0
 
 
+def test_adamw_scalars_that_are_infinite_in_32_bits_are_refused(K):
+    """Finite doubles whose rounding, or quotient with the bias correction, is no finite float: an element without a gradient would be NaN."""
+    def call(lr=1e-3, b1=0.9, decay=0.0, n=100, t=1):
+        a = (K.clt_adamw_tensor * 1)(K.clt_adamw_tensor(P, P, P, P, None, None, None, n, 0, 0, 32, decay))
+        return K._lib.clt_adamw_step(None, 1, a, t, lr, b1, 0.999, 1e-8, 0)
+    for bad in (dict(lr=1e39), dict(lr=1e300), dict(lr=1e38, b1=0.99), dict(lr=1e308, b1=0.999, n=0)):
+        refused(K, -1, "scalar", call(**bad))
+    refused(K, -1, "weight_decay", call(lr=1e10, decay=1e30))
+    for good in (dict(lr=1e38, b1=0.0, n=0), dict(lr=1e37, t=10 ** 6, n=0)):
+        assert call(**good) == 0
+
+
 def test_outputs_that_overlap_are_refused(K):
     at = lambda k: (k + 1) << 24      # places 16 MB apart
     L, B, d = 2, 3, 64
