@@ -40,3 +40,16 @@ RESTORE = "	s_mov_b64 exec, s[72:73]\n"
 ])
 def test_vector_work_without_lanes(behind, lost):
     assert B.vector_work_without_lanes(LOOP + behind + "	s_endpgm\n") == lost
+
+
+def test_a_branch_behind_an_or_of_the_lanes_ends_no_loop():
+    """`s_or exec, exec, saved` gives lanes back, so the branch on lanes behind it is taken and what follows it is another path's; every
+    other operation on EXEC in its place can have taken the last lane."""
+    body = "	v_mov_b32_e32 v53, v22\n" + RESTORE + "	s_endpgm\n"
+    for back in ("s_or_b64 exec, exec, s[2:3]", "s_or_b32 exec_lo, exec_lo, s2"):
+        assert B.vector_work_without_lanes(LOOP.replace("s_xor_b64 exec, exec, s[2:3]", back) + body) == []
+    for gone in ("s_xor_b64 exec, exec, s[2:3]", "s_and_b64 exec, exec, s[2:3]", "s_andn2_b64 exec, exec, s[2:3]", "s_mov_b64 exec, s[2:3]",
+                 "s_nor_b64 exec, exec, s[2:3]", "s_orn2_b64 exec, exec, s[2:3]"):
+        assert B.vector_work_without_lanes(LOOP.replace("s_xor_b64 exec, exec, s[2:3]", gone) + body) == [("row_kernel", "v_mov_b32_e32 v53, v22")], gone
+    # and a loop that ends with none is found behind one
+    assert B.vector_work_without_lanes("	s_or_b64 exec, exec, s[2:3]\n	s_cbranch_execnz .LBB21_28\n" + LOOP + body) == [("row_kernel", "v_mov_b32_e32 v53, v22")]
