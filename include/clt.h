@@ -267,7 +267,9 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  * itself), NULL without.  weight: [L,d] float.  Outputs, at least one of the first two: y [L,B,d] T; q [L,B,d] int8 with
  * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
  * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
- * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN gets codes 0 and a NaN as its scale.
+ * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN (an infinite sum x + residual among them) gets codes 0
+ * and a NaN as its scale.  A row of finite numbers has finite results whatever their size: where squares or products with the weights leave
+ * fp32, the row is scaled by a power of two before and rstd after.
  * 1 <= L <= 128, B >= 1, L B < 2^30, d <= 2^20 a positive multiple of 8,
  * eps > 0. */
 int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,

@@ -37,16 +37,24 @@ __device__ __forceinline__ u32x4 narrow16(const float (&f)[4]) {
   return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
 }
 
-// What the codes and the scale of a row follow from
-struct RowScale { float rstd, k, scale; bool broken; };
-__device__ __forceinline__ RowScale row_scale(float sum, uint32_t top, float eps, int d) {
+// A row whose sum of squares, or whose products with the weights, are beyond fp32 (some |h| is at least 2^54 then, or a weight beyond any use) is
+// divided by the power of two of its largest |h|, which is exact, and normalised in that form; only rstd gets the power back.  hmax: that |h|'s image.
+__device__ __forceinline__ bool beyond(float sum, uint32_t top) { return !(sum < __uint_as_float(0x7f800000u)) || top >= 0x7f800000u; }
+__device__ __forceinline__ float power_below(uint32_t hmax) {      // 2^-e, 2^-126 at the least; 1 where it would not help: an infinity, a NaN, a weight
+  return hmax < 0x3f800000u || hmax >= 0x7f800000u ? 1.f : __uint_as_float(max(254u - (hmax >> 23), 1u) << 23);
+}
+
+// What the codes and the scale of a row follow from; sum and top are those of the row times `down`
+struct RowScale { float norm, rstd, k, scale; bool broken; };
+__device__ __forceinline__ RowScale row_scale(float sum, uint32_t top, float eps, int d, float down) {
   RowScale r;
-  r.rstd = 1.0f / sqrtf(sum / (float)d + eps);
+  r.norm = 1.0f / sqrtf(sum / (float)d + eps * down * down);
+  r.rstd = r.norm * down;
   const float amax = __uint_as_float(top);
-  const bool zero = amax < ROW_IS_ZERO;
+  const bool zero = amax < fmaxf(ROW_IS_ZERO * down, 0x1p-118f);
   r.broken = top >= 0x7f800000u;
   r.k = r.broken || zero ? 0.f : 1.0f / amax * 127.0f;
-  r.scale = r.broken ? __uint_as_float(0x7fc00000u) : zero ? 1.f : amax * r.rstd / 127.0f;
+  r.scale = r.broken ? __uint_as_float(0x7fc00000u) : zero ? 1.f : amax * r.norm / 127.0f;
   return r;
 }
 __device__ __forceinline__ uint32_t code(float t, const RowScale& r) { return (uint32_t)(int)(r.broken ? 0.f : rintf(t * r.k)) & 255u; }
@@ -59,8 +67,8 @@ __device__ __forceinline__ uint32_t code(float t, const RowScale& r) { return (u
 template <typename T, int NV, int W, bool STREAM>
 __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_each, RmsNormArgs a) {
   constexpr int N = Vec16<T>::N;
-  __shared__ float sums[2][4];
-  __shared__ uint32_t tops[2][4];
+  __shared__ float sums[4][4];
+  __shared__ uint32_t tops[4][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = blockIdx.y;
   const int b0 = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x) * rows_each, b1 = min(B, b0 + rows_each);
   int e[NV];      // first element of each piece
@@ -87,8 +95,26 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
         if (a.residual) add[v] = take<STREAM, u32x4>(res + e[v]);
       }
     }
-    float t[NV][N], s = 0.f;
+    float t[NV][N], s = 0.f, down = 1.f;
     uint32_t top = 0;
+    auto measure = [&](const float (&h)[N], int v) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s = fmaf(h[i], h[i], s);
+        t[v][i] = h[i] * w[v][i];
+        top = max(top, __float_as_uint(t[v][i]) & 0x7fffffffu);
+      }
+    };
+    auto join = [&](int buf) __attribute__((always_inline)) {
+      s = wave_sum(s);
+      top = wave_max(top);
+      if (W == 4) {
+        if (lane == 0) { sums[buf][wave] = s; tops[buf][wave] = top; }
+        __syncthreads();
+        s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+        top = max(max(tops[buf][0], tops[buf][1]), max(tops[buf][2], tops[buf][3]));
+      }
+    };
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float h[N], r[N];
@@ -101,23 +127,37 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
         widen16(raw[v], h);
         if (e[v] < d) give<STREAM>(static_cast<T*>(a.h) + o + e[v], raw[v]);
       }
+      measure(h, v);
+    }
+    join(b & 1);      // (two buffers in turn: one barrier per row)
+    if (__builtin_expect(beyond(s, top), 0)) {      // (the same for all lanes of the row; it is read again, so that nobody else has to keep it)
+      const T* again = (a.residual ? static_cast<const T*>(a.h) : static_cast<const T*>(a.x)) + o;
+      auto load = [&](float (&h)[N], int v) __attribute__((always_inline)) {
+        widen16(e[v] < d ? *reinterpret_cast<const u32x4*>(again + e[v]) : u32x4{0u, 0u, 0u, 0u}, h);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        s = fmaf(h[i], h[i], s);
-        t[v][i] = h[i] * w[v][i];
-        top = max(top, __float_as_uint(t[v][i]) & 0x7fffffffu);
+        for (int i = 0; i < N; ++i) h[i] *= down;
+      };
+      s = 0.f;
+      top = 0;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float h[N];
+        load(h, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(h[i]) & 0x7fffffffu);
       }
+      join(2);
+      down = power_below(top);
+      top = 0;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float h[N];
+        load(h, v);
+        measure(h, v);
+      }
+      join(3);
     }
-    s = wave_sum(s);
-    top = wave_max(top);
-    if (W == 4) {
-      const int buf = b & 1;      // (two buffers: one barrier per row)
-      if (lane == 0) { sums[buf][wave] = s; tops[buf][wave] = top; }
-      __syncthreads();
-      s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
-      top = max(max(tops[buf][0], tops[buf][1]), max(tops[buf][2], tops[buf][3]));
-    }
-    const RowScale r = row_scale(s, top, a.eps, d);
+    const RowScale r = row_scale(s, top, a.eps, d, down);
     if ((W == 1 ? lane : threadIdx.x) == 0) {
       if (a.rstd) a.rstd[row] = r.rstd;
       if (a.q) a.q_scale[row] = r.scale;
@@ -128,7 +168,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
       if (a.y) {
         float y[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) y[i] = t[v][i] * r.rstd;
+        for (int i = 0; i < N; ++i) y[i] = t[v][i] * r.norm;
         give<STREAM>(static_cast<T*>(a.y) + o + e[v], narrow16(y));
       }
       if (a.q) {
@@ -145,44 +185,73 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(int B, int d, int rows_ea
 // Rows too wide for that: one workgroup per row, the row read twice.
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_wide_kernel(int B, int d, RmsNormArgs a) {
-  __shared__ float sums[4];
-  __shared__ uint32_t tops[4];
+  __shared__ float sums[2][4];
+  __shared__ uint32_t tops[3][4];
   const size_t row = blockIdx.x, o = row * d;
   const float* w = a.weight + row / B * d;
   const T* x = static_cast<const T*>(a.x) + o;
   T* hs = static_cast<T*>(a.h);
-  float s = 0.f;
+  const T* h = a.residual ? hs + o : x;
+  float s = 0.f, down = 1.f;
   uint32_t top = 0;
+  auto add = [&](float4 v, int i) __attribute__((always_inline)) {
+    const float4 w4 = *reinterpret_cast<const float4*>(w + i);
+    s = fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, fmaf(v.w, v.w, s))));
+    const uint32_t t0 = max(__float_as_uint(v.x * w4.x) & 0x7fffffffu, __float_as_uint(v.y * w4.y) & 0x7fffffffu);
+    const uint32_t t1 = max(__float_as_uint(v.z * w4.z) & 0x7fffffffu, __float_as_uint(v.w * w4.w) & 0x7fffffffu);
+    top = max(top, max(t0, t1));
+  };
+  auto largest = [&](int buf) __attribute__((always_inline)) {      // of all lanes' top
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) tops[buf][threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(tops[buf][0], tops[buf][1]), max(tops[buf][2], tops[buf][3]));
+  };
+  auto join = [&](int buf) __attribute__((always_inline)) {
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) sums[buf][threadIdx.x >> 6] = s;
+    largest(buf);
+    s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+  };
+  auto load = [&](int i) __attribute__((always_inline)) {
+    float4 v = Elem<T>::load4(h + i);
+    v.x *= down; v.y *= down; v.z *= down; v.w *= down;
+    return v;
+  };
   for (int i = threadIdx.x * 4; i < d; i += 1024) {
-    float4 h = Elem<T>::load4(x + i);
+    float4 v = Elem<T>::load4(x + i);
     if (a.residual) {
       const float4 r = Elem<T>::load4(static_cast<const T*>(a.residual) + o + i);
-      const typename Elem<T>::Raw4 raw = Elem<T>::narrow4(make_float4(h.x + r.x, h.y + r.y, h.z + r.z, h.w + r.w));
+      const typename Elem<T>::Raw4 raw = Elem<T>::narrow4(make_float4(v.x + r.x, v.y + r.y, v.z + r.z, v.w + r.w));
       *reinterpret_cast<typename Elem<T>::Raw4*>(hs + o + i) = raw;
-      h = Elem<T>::widen4(raw);
+      v = Elem<T>::widen4(raw);
     }
-    const float4 w4 = *reinterpret_cast<const float4*>(w + i);
-    s = fmaf(h.x, h.x, fmaf(h.y, h.y, fmaf(h.z, h.z, fmaf(h.w, h.w, s))));
-    const uint32_t t0 = max(__float_as_uint(h.x * w4.x) & 0x7fffffffu, __float_as_uint(h.y * w4.y) & 0x7fffffffu);
-    const uint32_t t1 = max(__float_as_uint(h.z * w4.z) & 0x7fffffffu, __float_as_uint(h.w * w4.w) & 0x7fffffffu);
-    top = max(top, max(t0, t1));
+    add(v, i);
   }
-  s = wave_sum(s);
-  top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6] = s; tops[threadIdx.x >> 6] = top; }
-  __syncthreads();
-  s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-  const RowScale r = row_scale(s, top, a.eps, d);
+  join(0);
+  if (__builtin_expect(beyond(s, top), 0)) {      // (the same for the whole workgroup)
+    top = 0;
+    for (int i = threadIdx.x * 4; i < d; i += 1024) {
+      const float4 v = load(i);
+      const uint32_t t0 = max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu);
+      top = max(top, max(t0, max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu)));
+    }
+    largest(2);
+    down = power_below(top);
+    s = 0.f;
+    top = 0;
+    for (int i = threadIdx.x * 4; i < d; i += 1024) add(load(i), i);
+    join(1);
+  }
+  const RowScale r = row_scale(s, top, a.eps, d, down);
   if (threadIdx.x == 0) {
     if (a.rstd) a.rstd[row] = r.rstd;
     if (a.q) a.q_scale[row] = r.scale;
   }
-  const T* h = a.residual ? hs + o : x;
   for (int i = threadIdx.x * 4; i < d; i += 1024) {
-    const float4 h4 = Elem<T>::load4(h + i), w4 = *reinterpret_cast<const float4*>(w + i);
+    const float4 h4 = load(i), w4 = *reinterpret_cast<const float4*>(w + i);
     const float t[4] = {h4.x * w4.x, h4.y * w4.y, h4.z * w4.z, h4.w * w4.w};
-    if (a.y) Elem<T>::store4(static_cast<T*>(a.y) + o + i, make_float4(t[0] * r.rstd, t[1] * r.rstd, t[2] * r.rstd, t[3] * r.rstd));
+    if (a.y) Elem<T>::store4(static_cast<T*>(a.y) + o + i, make_float4(t[0] * r.norm, t[1] * r.norm, t[2] * r.norm, t[3] * r.norm));
     if (a.q) *reinterpret_cast<uint32_t*>(a.q + o + i) = code(t[0], r) | code(t[1], r) << 8 | code(t[2], r) << 16 | code(t[3], r) << 24;
   }
 }

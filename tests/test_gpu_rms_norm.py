@@ -220,3 +220,48 @@ def test_binding_refusals_on_the_device():
             bad()
     torch.cuda.synchronize()
     assert torch.all(y == 5.0)
+
+
+# Rows whose squares, or whose products with the weights, are beyond fp32: every width that the kernels cut differently
+LARGE = [("bf16", 264), ("bf16", 776), ("bf16", 2048), ("bf16", 2056), ("bf16", 8192), ("bf16", 8200), ("f32", 136), ("f32", 1024), ("f32", 1032), ("f32", 4096), ("f32", 4104)]
+POWERS = (0, 30, 45, 58, 61, 63, 64, 65, 80, 100, 120, 124)
+
+
+def large_rows(dtype, d, seed):
+    """[2, 15, d]: normal numbers times powers of two; the type's largest number throughout, and once among ordinary ones; ordinary again."""
+    x = normal(seed, 2, len(POWERS) + 3, d)
+    x[:, :len(POWERS)] *= torch.tensor([2.0 ** k for k in POWERS])[:, None]
+    x = x.to(T[dtype])
+    top = torch.finfo(T[dtype]).max
+    x[:, len(POWERS)] = torch.where(normal(seed + 1, 2, d) > 0, top, -top).to(T[dtype])
+    x[:, len(POWERS) + 1, d // 3] = -top
+    return x, 1.0 + 0.3 * normal(seed + 2, 2, d)
+
+
+@pytest.mark.parametrize("dtype,d", LARGE)
+def test_rows_of_very_large_numbers(dtype, d):
+    from paper_2603_21014_amd import binding as K
+    x, w = large_rows(dtype, d, 70)
+    L, B, _ = x.shape
+    r = (x.float() * 0.25).to(T[dtype])
+    r[:, len(POWERS):len(POWERS) + 2] = 0.0      # (the sum of these stays finite)
+    for residual in (None, r):
+        h = torch.empty_like(x, device=DEV) if residual is not None else None
+        y, q = torch.empty_like(x, device=DEV), torch.empty(L, B, d, dtype=torch.int8, device=DEV)
+        s, rstd = torch.empty(L, B, device=DEV), torch.empty(L, B, device=DEV)
+        K.clt_rms_norm(x.to(DEV), w.to(DEV), EPS, y=y, q=q, q_scale=s, residual=None if residual is None else residual.to(DEV), h=h, rstd=rstd)
+        assert torch.isfinite(y).all() and torch.isfinite(s).all() and q.any(-1).all()
+        check_forward(x, residual, w, dtype, h, y, q, s, None)
+        want = R.rms_norm(np32(x), np64(w), EPS, None if residual is None else np32(residual), dtype == "bf16")[1]
+        assert np.all(np.abs(np64(rstd) - want) <= sums_bound(d) * want + 2.0 ** -149)      # (half a step of the smallest numbers, twice)
+    # a row with an infinity beside large numbers is still a broken one, and no row depends on another
+    again = x.clone()
+    again[:, 3, d - 1], again[:, 9, 0] = float("inf"), float("nan")
+    y2, q2, s2 = torch.empty_like(y), torch.empty_like(q), torch.empty_like(s)
+    K.clt_rms_norm(again.to(DEV), w.to(DEV), EPS, y=y2, q=q2, q_scale=s2)
+    K.clt_rms_norm(x.to(DEV), w.to(DEV), EPS, y=y, q=q, q_scale=s)
+    for b in range(B):
+        if b in (3, 9):
+            assert torch.isnan(s2[:, b]).all() and not q2[:, b].any()
+        else:
+            assert torch.equal(y[:, b], y2[:, b]) and torch.equal(q[:, b], q2[:, b]) and torch.equal(s[:, b], s2[:, b])
