@@ -281,7 +281,8 @@ int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, c
  *   dx = rstd (weight dy) - h rstd^3 mean(weight dy h) + dh,    dweight[l] = sum over the B rows of dy h rstd.
  * dx [L,B,d] T is the gradient of both x and residual; it may be dy or dh.  dweight: [L,d] float, or NULL when the
  * weights are not trained; with it, workspace (device, 16-byte aligned) of at least
- * clt_rms_norm_backward_workspace_bytes bytes, which nothing has to clear.  Sums in fp32, in a fixed order. */
+ * clt_rms_norm_backward_workspace_bytes bytes, which nothing has to clear.  Sums in fp32, in a fixed order; rows of very
+ * large numbers as in the forward pass. */
 int clt_rms_norm_backward_workspace_bytes(int32_t L, int32_t B, int32_t d, size_t* bytes);
 int clt_rms_norm_backward(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* h, const float* weight,
                           const float* rstd, const void* dy, const void* dh, void* dx, float* dweight, void* workspace,

@@ -258,6 +258,16 @@ __global__ __launch_bounds__(256) void rms_norm_wide_kernel(int B, int d, RmsNor
 
 // ---- backward pass ---------------------------------------------------------------------------------------------------
 //
+// Rows of very large numbers: with a small rstd its cube leaves fp32 (from 2^-42 on), and so do products of h and dy.  From 2^-30 on h is
+// multiplied by the power of two at or below rstd and rstd divided by it, both exact, so that the products are those of a row of ordinary
+// size; the factor of the projection gets the power back at its end.
+struct RowPower { float down, rn; };      // that power, rstd over it; 1 and rstd itself for ordinary rows
+__device__ __forceinline__ RowPower row_power(float rstd) {
+  if (!(rstd > 0.f && rstd < 0x1p-30f)) return {1.f, rstd};
+  const uint32_t e = max(__float_as_uint(rstd) >> 23, 1u);
+  return {__uint_as_float(e << 23), rstd * __uint_as_float((254u - e) << 23)};
+}
+
 // The same arrangement: h, dy (and dh) of a row are read once, for dx and for the row's share of dweight, which the lanes add up in
 // registers over all rows of their wavefront.  A workgroup leaves one partial sum of dweight, a second kernel adds those in order.
 // 16 layers of 4096 rows of 2048 in bf16 with dh (1.07 GB): 182 us, 5.9 TB/s; 300 rows of 2056: 4.5 us and 4.2 for the partial sums.
@@ -293,7 +303,18 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
         if (a.dh) re[v] = take<STREAM, u32x4>(static_cast<const T*>(a.dh) + o + e[v]);
       }
     }
-    const float r = a.rstd[row];
+    const float r = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(a.rstd[row])));      // (one row to a wavefront)
+    const RowPower p = row_power(r);
+    if (__builtin_expect(p.down != 1.f, 0)) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float h[N];
+        widen16(rh[v], h);
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] *= p.down;
+        rh[v] = narrow16(h);
+      }
+    }
     float s = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -304,7 +325,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
       for (int i = 0; i < N; ++i) {
         const float gh = g[i] * h[i];
         s = fmaf(w[v][i], gh, s);
-        dw[v][i] = fmaf(gh, r, dw[v][i]);
+        dw[v][i] = fmaf(gh, p.rn, dw[v][i]);
       }
     }
     s = wave_sum(s);
@@ -314,7 +335,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(int B, int d, in
       __syncthreads();
       s = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
     }
-    const float c = s / (float)d * r * r * r;
+    const float c = s / (float)d * p.rn * p.rn * p.rn * p.down;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float h[N], g[N], x[N];
@@ -360,17 +381,22 @@ __global__ __launch_bounds__(256) void rms_norm_dx_kernel(int B, int d, RmsNormB
   const float* w = a.weight + row / B * d;
   const T *h = static_cast<const T*>(a.h) + o, *dy = static_cast<const T*>(a.dy) + o;
   const float r = a.rstd[row];
+  const RowPower p = row_power(r);
+  auto load_h = [&](int i) __attribute__((always_inline)) {
+    const float4 v = Elem<T>::load4(h + i);
+    return make_float4(v.x * p.down, v.y * p.down, v.z * p.down, v.w * p.down);
+  };
   float s = 0.f;
   for (int i = threadIdx.x * 4; i < d; i += 1024) {
-    const float4 h4 = Elem<T>::load4(h + i), g4 = Elem<T>::load4(dy + i), w4 = *reinterpret_cast<const float4*>(w + i);
+    const float4 h4 = load_h(i), g4 = Elem<T>::load4(dy + i), w4 = *reinterpret_cast<const float4*>(w + i);
     s += (h4.x * (w4.x * g4.x) + h4.y * (w4.y * g4.y)) + (h4.z * (w4.z * g4.z) + h4.w * (w4.w * g4.w));
   }
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
   __syncthreads();
-  const float c = ((sums[0] + sums[1]) + (sums[2] + sums[3])) / (float)d * r * r * r;
+  const float c = ((sums[0] + sums[1]) + (sums[2] + sums[3])) / (float)d * p.rn * p.rn * p.rn * p.down;
   for (int i = threadIdx.x * 4; i < d; i += 1024) {
-    const float4 h4 = Elem<T>::load4(h + i), g4 = Elem<T>::load4(dy + i), w4 = *reinterpret_cast<const float4*>(w + i);
+    const float4 h4 = load_h(i), g4 = Elem<T>::load4(dy + i), w4 = *reinterpret_cast<const float4*>(w + i);
     float4 e = make_float4(0.f, 0.f, 0.f, 0.f);
     if (a.dh) e = Elem<T>::load4(static_cast<const T*>(a.dh) + o + i);
     Elem<T>::store4(static_cast<T*>(a.dx) + o + i,
@@ -391,7 +417,8 @@ __global__ __launch_bounds__(256) void rms_norm_dw_kernel(int B, int d, int rows
   float s = 0.f;
   for (int b = blockIdx.y * rows; b < end; ++b) {
     const size_t row = (size_t)l * B + b;
-    s = fmaf(Elem<T>::load(static_cast<const T*>(a.dy) + row * d + c) * a.rstd[row], Elem<T>::load(static_cast<const T*>(a.h) + row * d + c), s);
+    const RowPower p = row_power(a.rstd[row]);
+    s = fmaf(Elem<T>::load(static_cast<const T*>(a.dy) + row * d + c) * p.rn, Elem<T>::load(static_cast<const T*>(a.h) + row * d + c) * p.down, s);
   }
   a.part[((size_t)l * gridDim.y + blockIdx.y) * d + c] = s;
 }

@@ -265,3 +265,23 @@ def test_rows_of_very_large_numbers(dtype, d):
             assert torch.isnan(s2[:, b]).all() and not q2[:, b].any()
         else:
             assert torch.equal(y[:, b], y2[:, b]) and torch.equal(q[:, b], q2[:, b]) and torch.equal(s[:, b], s2[:, b])
+
+
+@pytest.mark.parametrize("dtype,d", LARGE)
+def test_gradients_of_rows_of_very_large_numbers(dtype, d):
+    from paper_2603_21014_amd import binding as K
+    x, w = large_rows(dtype, d, 80)
+    L, B, _ = x.shape
+    rstd = torch.from_numpy(R.rms_norm(np32(x), np64(w), EPS)[1]).float()
+    dy, e = (4.0 * normal(83, L, B, d)).to(T[dtype]), (2.0 ** -90 * normal(84, L, B, d)).to(T[dtype])
+    ws = torch.empty(K.clt_rms_norm_backward_workspace_bytes(L, B, d), dtype=torch.uint8, device=DEV)
+    for dh in (None, e):
+        dx, dw = torch.empty_like(x, device=DEV), torch.empty(L, d, device=DEV)
+        K.clt_rms_norm_backward(x.to(DEV), w.to(DEV), rstd.to(DEV), dy.to(DEV), dx, dw, ws, dh=None if dh is None else dh.to(DEV))
+        want_dx, want_dw = R.rms_norm_backward(np32(x), np64(w), np64(rstd), np32(dy), None if dh is None else np32(dh))
+        h, g, r = np64(x), np64(dy), np64(rstd)[..., None]
+        wg = np.abs(np64(w)[:, None, :] * g)
+        size = r * wg + np.abs(h) * r ** 3 * (wg * np.abs(h)).mean(-1, keepdims=True) + (0 if dh is None else np.abs(np64(dh)))
+        # (1e-38: results among the smallest numbers, where a step is not relative to the value)
+        assert np.all(np.abs(np64(dx) - want_dx) <= HALF[dtype] * np.abs(want_dx) + size * sums_bound(d) * 1.01 + 1e-38)
+        assert np.all(np.abs(np64(dw) - want_dw) <= (np.abs(g * h * r)).sum(1) * (B + 8) * U)
