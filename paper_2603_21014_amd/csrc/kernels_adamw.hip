@@ -166,29 +166,37 @@ template <bool ROW, bool WHOLE, bool STREAM> __device__ __forceinline__ void sto
   if (t.bf16) store8<ROW, WHOLE, STREAM>(static_cast<bf16_t*>(t.p) + i0, left, p);
   else store8<ROW, WHOLE, STREAM>(static_cast<float*>(t.p) + i0, left, p);
 }
-__device__ __forceinline__ void update(float (&p)[8], float (&m)[8], float (&v)[8], const float (&g)[8], float keep, const AdamScalars& a) {
+// The square root's unit takes denormal numbers for zeros.  Beside an eps of 2^-39 and more the root of one, below 2^-63, is less than
+// the sum's rounding; beside a smaller eps (SMALL) it decides the step, and small arguments are scaled by 2^64.
+constexpr float SMALL_EPS = 0x1p-39f;
+template <bool SMALL> __device__ __forceinline__ float root(float x) {
+  if (!SMALL) return __builtin_amdgcn_sqrtf(x);
+  const bool low = x < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(low ? x * 0x1p64f : x) * (low ? 0x1p-32f : 1.f);
+}
+template <bool SMALL> __device__ __forceinline__ void update(float (&p)[8], float (&m)[8], float (&v)[8], const float (&g)[8], float keep, const AdamScalars& a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     update_moments(m[i], v[i], g[i], a);
     // (square root and reciprocal: one unit each, as in adam_element)
-    const float den = __builtin_amdgcn_sqrtf(v[i] * a.inv_bc2) + a.eps;
+    const float den = root<SMALL>(v[i] * a.inv_bc2) + a.eps;
     p[i] = fmaf(a.neg_lr_over_bc1 * m[i], __builtin_amdgcn_rcpf(den), p[i] * keep);
   }
 }
 
-template <bool WHOLE, bool STREAM> __device__ __forceinline__ void chunk32(const AdamWTensor& t, int64_t base, const AdamScalars& a) {
+template <bool WHOLE, bool STREAM, bool SMALL> __device__ __forceinline__ void chunk32(const AdamWTensor& t, int64_t base, const AdamScalars& a) {
   const int64_t i0 = base + threadIdx.x * 4, left = t.n - i0;
   float g[8], p[8], m[8], v[8];
   load_gp<false, WHOLE, STREAM>(t, i0, g, p);
   load8<false, WHOLE, STREAM>(static_cast<const float*>(t.m) + i0, left, m);
   load8<false, WHOLE, STREAM>(static_cast<const float*>(t.v) + i0, left, v);
-  update(p, m, v, g, t.keep, a);
+  update<SMALL>(p, m, v, g, t.keep, a);
   store8<false, WHOLE, STREAM>(static_cast<float*>(t.m) + i0, left, m);
   store8<false, WHOLE, STREAM>(static_cast<float*>(t.v) + i0, left, v);
   store_p<false, WHOLE, STREAM>(t, i0, p);
 }
 
-template <bool WHOLE, bool STREAM> __device__ __forceinline__ void chunk8(const AdamWTensor& t, int64_t base, const AdamScalars& a) {
+template <bool WHOLE, bool STREAM, bool SMALL> __device__ __forceinline__ void chunk8(const AdamWTensor& t, int64_t base, const AdamScalars& a) {
   const int64_t i0 = base + threadIdx.x * 8, left = t.n - i0;
   const int64_t block = (WHOLE || left > 0 ? i0 : base) / CLT_ADAMW_BLOCK;      // (lanes behind the end: any block; they hold zeros)
   float g[8], p[8], m[8], v[8];
@@ -199,7 +207,7 @@ template <bool WHOLE, bool STREAM> __device__ __forceinline__ void chunk8(const 
   const float mf = scale_value(ms), vf = scale_value(vs);
   decode_m(mc[0], mf, m); decode_m(mc[1], mf, m + 4);
   decode_v(vc[0], vf, v); decode_v(vc[1], vf, v + 4);
-  update(p, m, v, g, t.keep, a);
+  update<SMALL>(p, m, v, g, t.keep, a);
   uint32_t mtop = 0, vtop = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -227,7 +235,7 @@ template <bool WHOLE, bool STREAM> __device__ __forceinline__ void chunk8(const 
 }
 
 // One workgroup per ADAMW_CHUNK elements of one tensor.
-template <bool STREAM>
+template <bool STREAM, bool SMALL>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamWList q) {
   int k = 0;
   while (k + 1 < q.count && q.t[k + 1].chunk0 <= blockIdx.x) ++k;
@@ -235,11 +243,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWList q) {
   const int64_t base = (int64_t)(blockIdx.x - t.chunk0) * ADAMW_CHUNK;
   const bool whole = base + ADAMW_CHUNK <= t.n;
   if (t.state8) {
-    if (whole) chunk8<true, STREAM>(t, base, q.a);
-    else chunk8<false, STREAM>(t, base, q.a);
+    if (whole) chunk8<true, STREAM, SMALL>(t, base, q.a);
+    else chunk8<false, STREAM, SMALL>(t, base, q.a);
   } else {
-    if (whole) chunk32<true, STREAM>(t, base, q.a);
-    else chunk32<false, STREAM>(t, base, q.a);
+    if (whole) chunk32<true, STREAM, SMALL>(t, base, q.a);
+    else chunk32<false, STREAM, SMALL>(t, base, q.a);
   }
 }
 
@@ -255,8 +263,11 @@ hipError_t launch_adamw(hipStream_t s, const AdamWList& q) {
     const AdamWTensor& t = q.t[i];
     bytes += (double)t.n * ((t.bf16 ? 2 : 4) + (t.grad_bf16 ? 2 : 4) + (t.state8 ? 2 : 8) + (t.master ? 4 : 0));
   }
-  if (bytes > 256e6) hipLaunchKernelGGL(adamw_kernel<true>, dim3(q.chunks), dim3(256), 0, s, q);
-  else hipLaunchKernelGGL(adamw_kernel<false>, dim3(q.chunks), dim3(256), 0, s, q);
+  const bool stream = bytes > 256e6, small = q.a.eps < SMALL_EPS;
+  if (stream && small) hipLaunchKernelGGL((adamw_kernel<true, true>), dim3(q.chunks), dim3(256), 0, s, q);
+  else if (stream) hipLaunchKernelGGL((adamw_kernel<true, false>), dim3(q.chunks), dim3(256), 0, s, q);
+  else if (small) hipLaunchKernelGGL((adamw_kernel<false, true>), dim3(q.chunks), dim3(256), 0, s, q);
+  else hipLaunchKernelGGL((adamw_kernel<false, false>), dim3(q.chunks), dim3(256), 0, s, q);
   return hipGetLastError();
 }
 

@@ -243,3 +243,21 @@ def test_tensors_that_get_other_memory_leave_the_list_its_own():
     opt.step(1, 1e-3)
     torch.cuda.synchronize()
     assert torch.all(p == 7.0) and all(torch.all(t == 5.0) for t in other)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_second_moments_among_the_smallest_numbers(bits):
+    """Gradients around 1e-20 with an eps far below them: v' is a denormal number, and its root still decides the step."""
+    from paper_2603_21014_amd import binding as K
+    n, eps = 1000, 1e-30
+    c = Case(K, n, "f32", "f32", bits, decay=0.0, seed=14, started=False)
+    c.g = (1e-20 * np.sign(np32(normal(15, n))) * (1 + np.abs(np32(normal(16, n))))).astype(np.float32)
+    c.dg.t.copy_(torch.from_numpy(c.g))
+    K.AdamW([c.c], B1, B2, eps, SEED).step(1, LR)
+    o = R.adamw(c.p, c.g, c.m, c.v, 1, LR, B1, B2, eps, 0.0, c.ms, c.vs, SEED, 0)
+    assert o["v32"].max() < 2.0 ** -126 and o["v32"].min() > 2.0 ** -149 * 8
+    step = np.abs(c.p - o["p"])
+    # v' / (1 - beta2) is rounded to a number of spacing 2^-149: half of that relative to it, and half again in the root
+    v_hat = o["v32"].astype(np.float64) / (1 - B2)
+    assert np.all(np.abs(np64(c.dp.t) - o["p"]) <= step * (16 * U + 2.0 ** -151 / v_hat) + np.abs(c.p) * 3 * U)
+    assert step.max() < 1.1 * LR
