@@ -261,3 +261,28 @@ def test_second_moments_among_the_smallest_numbers(bits):
     v_hat = o["v32"].astype(np.float64) / (1 - B2)
     assert np.all(np.abs(np64(c.dp.t) - o["p"]) <= step * (16 * U + 2.0 ** -151 / v_hat) + np.abs(c.p) * 3 * U)
     assert step.max() < 1.1 * LR
+
+
+def test_moves_as_the_existing_adam_step_does():
+    """In fp32 storage, where a step is far above the storage's rounding: three steps of both from the same state."""
+    from paper_2603_21014_amd import binding as K
+    L, d, F, B, lr = 2, 64, 136, 8, 1e-3
+    step = K.CLTStep(L, d, F, B, dtype="f32", device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    params = {k: torch.randn(s.shape, generator=g, device=DEV) for k, s in step.grads.items()}
+    start = {k: p.clone() for k, p in params.items()}
+    mine = {k: p.clone() for k, p in params.items()}
+    m, v = ({k: torch.zeros_like(p) for k, p in params.items()} for _ in range(2))
+    opt = K.AdamW([K.AdamWTensor(mine[k], step.grads[k], *K.AdamW.moments(mine[k])) for k in params])
+    for t in (1, 2, 3):
+        for k in step.grads:
+            step.grads[k].copy_(1e-2 * torch.randn(step.grads[k].shape, generator=g, device=DEV))
+        step.adam_step(t, lr, params, m, v)
+        opt.step(t, lr)
+    for k in params:
+        moved = (params[k] - start[k]).abs()
+        # the existing step forms 1 - beta from the rounded betas: up to 2.4e-7 of m and 4e-5 of v, half of that in the root, so 2.1e-5 of each
+        # step of at most about lr; and each of three additions to a parameter rounds by half a step, on both sides
+        bound = 3 * lr * 3e-5 + 6 * U * params[k].abs()
+        assert torch.all((params[k] - mine[k]).abs() <= bound)
+        assert (moved > 20 * bound).float().mean() > 0.95

@@ -302,6 +302,26 @@ def test_second_moment_in_8_bits_follows_the_gradient():
     assert seen.std() < 0.6
 
 
+def test_second_moment_in_8_bits_follows_the_gradient_at_a_memory_of_1000_steps():
+    """The same at beta2 = 0.999, where v moves by a thousandth of itself in a step: 6000 steps, the last 3000 looked at."""
+    rng = np.random.default_rng(12)
+    n, b2 = 512, 0.999
+    m, v, ms, vs = np.zeros(n, np.uint8), np.zeros(n, np.uint8), np.zeros(n // 128, np.uint8), np.zeros(n // 128, np.uint8)
+    total, square = np.zeros(n), 0.0
+    for t in range(1, 6001):
+        o = R.adamw(np.zeros(n), (3e-4 * rng.normal(size=n)).astype(np.float32), m, v, t, 0.0, 0.9, b2, 1e-8, 0.0, ms, vs, 6, 1)
+        m, v, ms, vs = o["m"], o["v"], o["m_scale"], o["v_scale"]
+        if t > 3000:
+            x = R.decode_moments(v, vs, R.E5M2, False).astype(np.float64) / 9e-8 / (1.0 - b2 ** t)
+            total += x
+            square += (x * x).mean()
+    mean = total.mean() / 3000
+    # rounding to a neighbour: variance (grid step) * |drift| = 0.19 * 0.001 * E|g^2 - 1| (0.97) = 1.8e-4 a step, over 2 * 0.001: 0.092, and 0.001 of
+    # the gradients' own; over 512 elements and 3 memories, with a correlation over two of them: sqrt(0.093 * 2 / 3 / 512) = 0.011
+    assert abs(mean - 1.0) < 5 * 0.011, mean
+    assert np.sqrt(square / 3000 - mean ** 2) < 0.45      # (0.31 expected)
+
+
 def test_oracle_mx4_packing_and_rounding():
     rng = np.random.default_rng(9)
     a = (rng.normal(size=(2, 70, 200)) * np.exp(2 * rng.normal(size=(2, 70, 1)))).astype(np.float32)
