@@ -329,7 +329,7 @@ int clt_adamw_step(void* stream, int32_t n_tensors, const clt_adamw_tensor* tens
  * negatives), and for every 32 consecutive elements along the contraction a power of two 2^(s-127), s one byte (E8M0).
  * s is the smallest for which no element is off by more than half a step: with max|a| = 2^e f, 1 <= f < 2, s - 127 = e - 2 for
  * f < 1.75 and e - 1 above (not below 2^-127).  Elements are rounded to nearest, ties to even.  A block with an infinity or a
- * NaN gets s = 255: its products are NaN.
+ * NaN gets s = 255: its values and its products are NaN (which clt_mx4_product's threshold turns into 0, see there).
  *
  * A packed matrix of [L][rows][K] (K along the contraction) is two arrays, in the order in which the matrix cores read
  * them; KS = ceil(K / 128) steps, RP = ceil(rows / 64) panels:
@@ -351,7 +351,10 @@ int clt_mx4_dequantise(void* stream, int32_t L, int32_t rows, int32_t K, int32_t
 /* out[l] = A[l] B[l]^T + bias[l], with theta kept where it is > theta[l] and 0 elsewhere: with A the packed activations
  * (M tokens) and B the packed W_enc (N = F features), the encoder and JumpReLU of eq. 1 on 4-bit operands, for passes that
  * only need features.  A is [L][M][K], B [L][N][K], bias and theta [L][N] float or NULL, out [L][M][N] of T; N a
- * multiple of 8.  Accumulated in fp32; the comparison is made before the rounding to T. */
+ * multiple of 8.  Accumulated in fp32; the comparison is made before the rounding to T.  A NaN is not > theta: as in
+ * clt_forward it becomes 0, so that a broken operand shows in the results without theta, and in its scales (255), but not in
+ * features.  theta is the threshold itself: with clt_config.log_threshold, whose theta tensor holds log(theta), the caller passes its
+ * exponential; TopK (CLT_ACT_TOPK) selects among the results without theta. */
 int clt_mx4_product(void* stream, int32_t L, int32_t M, int32_t N, int32_t K, const void* a_codes, const void* a_scales,
                     const void* b_codes, const void* b_scales, const float* bias, const float* theta, int32_t dtype, void* out);
 

@@ -492,7 +492,8 @@ def clt_mx4_dequantise(codes, scales, out):
 
 
 def clt_mx4_product(a_codes, a_scales, b_codes, b_scales, out, K, bias=None, theta=None):
-    """out [L, M, N] = A B^T + bias of packed A [L][M][K] and B [L][N][K], with theta kept where above it, else 0."""
+    """out [L, M, N] = A B^T + bias of packed A [L][M][K] and B [L][N][K], with theta kept where above it, else 0 (a NaN too).
+    theta is the threshold itself: of a step with log_threshold it is params["theta"].exp()."""
     dev = _device_of(out, "out")
     dt, s, f32 = _storage(out, "out"), out.shape, torch.float32
     L, M, N = s

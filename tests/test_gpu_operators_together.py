@@ -120,3 +120,29 @@ def test_adamw_asks_for_the_matrices_gradients():
     step = K.CLTStep(L, d, F, B, device=DEV, matrix_grads=False)
     with pytest.raises(ValueError):
         step.adamw({})
+
+
+def test_threshold_of_the_encoder_in_4_bits_is_that_of_the_step():
+    """On operands that 4 bits hold exactly: the same features as clt_forward's, with the threshold held as its logarithm, and none of a token
+    that is broken."""
+    from paper_2603_21014_amd import binding as K
+    g = torch.Generator().manual_seed(9)
+    values = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    some = lambda *s: values[torch.randint(0, 8, s, generator=g)] * (1 - 2 * torch.randint(0, 2, s, generator=g))
+    x, w = some(L, B, d), some(L, d, F)
+    x[:, :, ::32], w[:, ::32, :] = 6.0, -6.0      # (every block reaches the largest number, so that its scale is 1)
+    x[1, 5, 40] = float("nan")
+    params = {"W_enc": w.bfloat16().to(DEV), "b_enc": torch.zeros(L, F, device=DEV), "theta": torch.full((L, F), 4.5, device=DEV).log(),
+              "W_dec": torch.zeros(L * (L + 1) // 2, F, d, dtype=torch.bfloat16, device=DEV), "b_dec": torch.zeros(L, d, device=DEV)}
+    step = K.CLTStep(L, d, F, B, log_threshold=True, device=DEV)
+    xd = x.bfloat16().to(DEV)
+    step.forward(xd, params)
+    wc, ws = K.mx4_empty(L, F, d)
+    xc, xs = K.mx4_empty(L, B, d)
+    K.clt_mx4_quantise(params["W_enc"], wc, ws, transposed=True)
+    K.clt_mx4_quantise(xd, xc, xs)
+    z = torch.empty(L, B, F, dtype=torch.bfloat16, device=DEV)
+    K.clt_mx4_product(xc, xs, wc, ws, z, d, theta=params["theta"].exp())
+    # (products are multiples of 1/4 and sums below 2^14: exact in fp32, and none is at the threshold's rounding)
+    assert torch.equal(z, step.z) and (z != 0).any() and not torch.isnan(z).any()
+    assert not z[1, 5].any() and xs.eq(255).any()
