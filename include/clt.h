@@ -123,7 +123,10 @@ typedef struct clt_config {
                              longer goes backward through the dense kernels.                */
   float C;                /* sparsity scale C of the App. B objective                     */
   float ste_bandwidth;    /* width eps of the rectangle kernel of the threshold gradient */
-  float beta1, beta2, adam_eps; /* Adam (App. C Table 1: 0.9, 0.999)                     */
+  float beta1, beta2, adam_eps; /* Adam (App. C Table 1: 0.9, 0.999).  Of clt_adam_step and
+                             clt_backward_adam_step: corrected second moments below 2^-126
+                             (gradients below 1e-19) count as zeros, which an adam_eps of 2^-39
+                             (1.8e-12) and more leaves without effect.                       */
 } clt_config;
 
 /* The five learned tensors, or things shaped like them (gradients, moments). */

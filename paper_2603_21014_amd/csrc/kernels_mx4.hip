@@ -88,8 +88,9 @@ template <> struct Eight<int8_t> {
 // Rows along the contraction.  A wavefront packs 16 rows by one step (1 KB of codes): four lanes share a block, eight elements each, so
 // loads are 16 bytes of bf16 per lane and a block's largest element is two maxima inside a quad away; its four blocks of a row come
 // one after the other, their loads in flight together.  A workgroup is a panel of 64 rows (whose scales share 256 bytes) by
-// QUANTISE_STEPS steps.  Bound by memory: 16 layers of 4096 rows of 2048 bf16 (340 MB) 60 us, 5.7 TB/s (64 us with one step); small calls by the
-// instructions, about seven an element: 6 layers of 1037 int8 rows of 2056 8.4 us.
+// QUANTISE_STEPS steps.  Bound by memory: 16 layers of 4096 rows of 2048 bf16 (340 MB) 60 us, 5.7 TB/s (64 us with one step).  Small calls are not: 6 layers of
+// 1037 int8 rows of 2056 (20 MB) take 8.4 us, twice their bytes' time, in about seven instructions an element, the maximum and the exchange inside a
+// quad among them.
 constexpr int QUANTISE_STEPS = 2;
 template <typename TE>
 __global__ __launch_bounds__(256) void mx4_quantise_kernel(int rows, int K, int KS, int chunks, const TE* __restrict__ a,
@@ -348,17 +349,18 @@ __device__ __forceinline__ void finish(const ProductArgs& p, int l, int token0, 
 // features by all the tokens (8 x 4 accumulators of 16 x 16).  A panel is read by one wavefront only and goes from memory into its
 // registers, one step ahead; the tokens are fetched three steps ahead and staged in LDS, in three stages of one step each.  Both run on
 // into the next tile.  Two workgroups share a compute unit, so that one's epilogue runs under the other's matrix instructions.
-// Measured: 16 layers of 4096 by 8192 by K = 2048 610 us, 3.6 PFLOP/s (bare loop of the instruction on random operands 7.2, with the LDS reads and the barrier
-// 6.5); at K = 32768 4.5 on random numbers and 5.3 on zeros, where power is no limit.  What bounds it besides power: the operands' way through the vector cache,
-// 64 bytes a cycle.  A wavefront's step takes 6.75 KB that way, which is 860 cycles for the eight of a compute unit, beside 1024 of matrix instructions (the
-// LDS, 256 bytes a cycle, is busy 40 %).  The same shape with half of the features' loads left out 600 us in a run where it took 632, without them 566, without the
-// tokens' as well 533.  A tile of 128 by 128 to a wavefront would need a third fewer operands and all registers of a SIMD, with no second
-// workgroup for the epilogue to hide under.
+// Measured: 16 layers of 4096 by 8192 by K = 2048, bf16 results, 590 to 610 us in a loop of 100 (two cards), 3.6 to 3.7 PFLOP/s, and 615 to 660 behind other work;
+// fp32 results 739.  A bare loop of the instruction on random operands reaches 7.2, with the LDS reads and the barrier 6.5; at K = 32768 this kernel 4.5 on random
+// numbers and 5.3 on zeros, where power is no limit.  No one unit bounds it: of the cycles of a step, 1024 are matrix instructions of a compute unit's eight
+// wavefronts, 860 the operands' way through the vector cache (64 bytes a cycle, 6.75 KB a wavefront), 40 % the LDS, and they do not overlap altogether.  With
+// parts left out, of 632 us in that run: half of the features' loads 600, the scales' 602, all of the features' 566, the tokens' as well 533; with all loads,
+// of 619: no stores 551, nor the results' way through LDS 534, nor the threshold 519, and that on zeros 443.  A tile of 128 by 128 to a wavefront would need a third fewer
+// operands and all registers of a SIMD, with no second workgroup for the epilogue to hide under.
 constexpr int PT = 8;             // tiles of 16 tokens
 constexpr int AHEAD = 3;          // of these, the operands under way from LDS
 constexpr int WORKGROUPS = 512;   // two on each of 256 compute units
 
-// Quotients n / d for n < 2^31 by a multiplication: m = floor(2^(31+s) / d) + 1 with 2^(s-1) < d <= 2^s is too large by less than 2^s / 2^(31+s)
+// Quotients n / d for n < 2^31 by a multiplication (Granlund and Montgomery's division by invariant integers): m = floor(2^(31+s) / d) + 1 with 2^(s-1) < d <= 2^s is too large by less than 2^s / 2^(31+s)
 // of itself.  (Division instructions do not exist; a wavefront would spend as long on three quotients as on two steps.)
 struct Quotient {
   uint32_t m, s;
@@ -641,7 +643,8 @@ hipError_t launch_product(hipStream_t s, int L, const ProductArgs& p) {
   // The kernel for few tokens: up to 32 of them, and where tiles are too few for the chip.  us with it and with the other one (L, M, N, K):
   // 16, 1, 8192, 2048 22.0 / 22.4; 1, 64, 8192, 2048 (32 tiles) 4.9 / 11.2; 1, 300, 2048, 8192 (24) 11.1 / 32.7; 4, 128, 6144, 768 (96) 6.5 / 8.3;
   // 1, 512, 8192, 2048 (128) 12.2 / 13.0; 1, 768, 8192, 2048 (192) 17.2 / 13.6; 8, 128, 8192, 2048 (256) 22.3 / 14.9; 12, 64, 6144, 768 (288) 8.7 / 10.2;
-  // 16, 48, 8192, 2048 (512) 25.5 / 24.5.  Two tiles of tokens instead of one at 17 to 32 tokens: 12 layers of 6144, K = 768 6.2 and 6.6.
+  // 16, 48, 8192, 2048 (512) 25.5 / 24.5.  (The rule counts tiles, not how full they are: at 33 to 64 tokens of few steps, as in the last but one, the
+  // kernel that is taken is the slower one.)  Two tiles of tokens instead of one at 17 to 32 tokens: 12 layers of 6144, K = 768 6.2 and 6.6.
   if (p.M <= 16) {
     hipLaunchKernelGGL((mx4_product_few_kernel<T, THETA, 1>), dim3(panels_n, 1, L), dim3(256), 0, s, p);
     return hipGetLastError();
