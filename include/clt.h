@@ -271,8 +271,8 @@ int clt_backward_adam_step(clt_handle* handle, void* stream,
  * q_scale [L,B] float, the format CLT_INPUT_INT8_ROWSCALE: q = rint(127 y / max|y|), q_scale = max|y| / 127 (both from
  * unrounded y); rstd [L,B] float (may be NULL), what the backward pass needs.  A row whose largest |h weight| is
  * below 2^-100 gets codes 0 and scale 1.  A row that holds an infinity or a NaN (an infinite sum x + residual among them) gets codes 0
- * and a NaN as its scale.  A row of finite numbers has finite results whatever their size: where squares or products with the weights leave
- * fp32, the row is scaled by a power of two before and rstd after.
+ * and a NaN as its scale.  Finite numbers may have any size: where their squares or products with the weights leave fp32, the row is scaled
+ * by a power of two before and rstd after.
  * 1 <= L <= 128, B >= 1, L B < 2^30, d <= 2^20 a positive multiple of 8,
  * eps > 0. */
 int clt_rms_norm(void* stream, int32_t L, int32_t B, int32_t d, int32_t dtype, const void* x, const void* residual,
@@ -317,6 +317,7 @@ typedef struct clt_adamw_tensor {
  * in one launch for every 32 of them:
  *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + ((1 - beta2) g) g,
  *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^t) m' / (sqrt(v' / (1 - beta2^t)) + eps).
+ * In fp32: gradients below 1e-22 leave no trace in v, and under those above 1e19 a v' / (1 - beta2^t) out of range makes no step.
  * The update uses m' and v' before they are rounded.  8-bit moments are rounded to one of their two neighbours at
  * random, without bias: with beta2 = 0.999, v moves by a thousandth of itself in a step and a step of E5M2 is 14 to 25 %, so
  * that rounding to nearest would never let it move; and because the scales are powers of two, a value that stays

@@ -37,11 +37,11 @@ __device__ __forceinline__ u32x4 narrow16(const float (&f)[4]) {
   return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
 }
 
-// A row whose sum of squares, or whose products with the weights, are beyond fp32 (some |h| is at least 2^54 then, or a weight beyond any use) is
-// divided by the power of two of its largest |h|, which is exact, and normalised in that form; only rstd gets the power back.  hmax: that |h|'s image.
+// A row whose sum of squares, or whose products with the weights, are beyond fp32 is multiplied by the power of two that brings its largest |h|
+// into [1/2, 1), which is exact, and normalised in that form, where no product is above its weight; only rstd gets the power back.  hmax: that |h|'s image.
 __device__ __forceinline__ bool beyond(float sum, uint32_t top) { return !(sum < __uint_as_float(0x7f800000u)) || top >= 0x7f800000u; }
-__device__ __forceinline__ float power_below(uint32_t hmax) {      // 2^-e, 2^-126 at the least; 1 where it would not help: an infinity, a NaN, a weight
-  return hmax < 0x3f800000u || hmax >= 0x7f800000u ? 1.f : __uint_as_float(max(254u - (hmax >> 23), 1u) << 23);
+__device__ __forceinline__ float power_below(uint32_t hmax) {      // 1 where it would not help: an infinity, a NaN, a weight that is one
+  return hmax < 0x3f800000u || hmax >= 0x7f800000u ? 1.f : __builtin_amdgcn_ldexpf(1.f, 126 - (int)(hmax >> 23));
 }
 
 // What the codes and the scale of a row follow from; sum and top are those of the row times `down`

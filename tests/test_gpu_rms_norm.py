@@ -285,3 +285,18 @@ def test_gradients_of_rows_of_very_large_numbers(dtype, d):
         # (1e-38: results among the smallest numbers, where a step is not relative to the value)
         assert np.all(np.abs(np64(dx) - want_dx) <= HALF[dtype] * np.abs(want_dx) + size * sums_bound(d) * 1.01 + 1e-38)
         assert np.all(np.abs(np64(dw) - want_dw) <= (np.abs(g * h * r)).sum(1) * (B + 8) * U)
+
+
+@pytest.mark.parametrize("dtype,d", LARGE)
+def test_rows_under_very_large_weights(dtype, d):
+    """Rows of one size throughout, whose norm is 1, so that y is the weight: finite, while h weight is not."""
+    from paper_2603_21014_amd import binding as K
+    powers = (0, 1, 10, 53, 70, 126, 127)
+    sign = torch.where(normal(90, 1, len(powers), d) > 0, 1.0, -1.0)
+    x = (sign * torch.tensor([1.9375 * 2.0 ** k for k in powers])[:, None]).to(T[dtype])      # (5 bits: exact in bf16)
+    w = torch.full((1, d), 3e38) * (1 - 0.25 * torch.rand((1, d), generator=torch.Generator().manual_seed(91)))
+    y, q = torch.empty_like(x, device=DEV), torch.empty(1, len(powers), d, dtype=torch.int8, device=DEV)
+    s = torch.empty(1, len(powers), device=DEV)
+    K.clt_rms_norm(x.to(DEV), w.to(DEV), EPS, y=y, q=q, q_scale=s)
+    assert torch.isfinite(y).all() and torch.isfinite(s).all() and (q != 0).all()
+    check_forward(x, None, w, dtype, None, y, q, s, None)
